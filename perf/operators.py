@@ -318,9 +318,7 @@ def _own(s):
 
     c = s["case"]
     if c["op"] == "linear":
-        B.mx4_quantize(s["x"], s["x_codes"], s["x_scales"])
-        B.mx4_linear(s["x_codes"], s["x_scales"], s["own_codes"], s["own_scales"], s["out"], bias=s["bias"], relu=c["relu"])
-        return s["out"]
+        return B.mx4_linear(s["x"], s["w"], s["out"], bias=s["bias"], relu=c["relu"])
     cache = s["cache"]
     if c["op"] == "attention":
         cache.attention(s["q"], s["out"], offsets=s["offsets"], window=c["window"], sinks=c["sinks"])
@@ -410,8 +408,7 @@ def prepare(case, seed):
         s["bias"] = torch.randn(n, generator=g, device=dev) * 0.01
         if own:
             from paper_2511_12934_b200 import binding as B
-            s["own_codes"], s["own_scales"] = B.mx4_quantize(w)
-            s["x_codes"], s["x_scales"] = B.mx4_empty(m, k)
+            s["w"] = B.mx4_quantize(w)
         s["out"] = torch.empty(m, n, dtype=dt, device=dev)
         return s
     L, R, n = _lengths(c), c["page_rows"], c["seqs"]
