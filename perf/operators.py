@@ -465,8 +465,8 @@ def _exact_values(x):
     """What x stands for after quantisation to 4 bits, from the definition: nearest representable multiples of each block's scale."""
     b = x.double().reshape(*x.shape[:-1], -1, 32)
     top = b.abs().amax(-1, keepdim=True)
-    exponent = torch.frexp(torch.where(top > 0, top, torch.ones_like(top))).exponent.double() - 1 - 2
-    scale = torch.where(top > 0, 2.0 ** exponent.clamp(min=-127), torch.full_like(top, 2.0 ** -127))
+    exponent = torch.where(top > 0, torch.frexp(top).exponent - 1 - 2, torch.full_like(top, -127).int()).clamp(min=-127)
+    scale = torch.ldexp(torch.ones_like(top), exponent)
     y = (b / scale).abs()
     step = torch.where(y >= 4, 2.0, torch.where(y >= 2, 1.0, 0.5)).double()
     y = (torch.round(y / step) * step).clamp(max=6.0)
@@ -477,7 +477,7 @@ def _exact_stored(codes, scales):
     v = torch.tensor(VALUES, dtype=torch.float64, device=codes.device)
     halves = [torch.where(h >= 8, -v[(h % 8).long()], v[(h % 8).long()]) for h in (codes % 16, codes // 16)]
     x = torch.stack(halves, -1).reshape(*scales.shape, 32)
-    return (x * (2.0 ** (scales.double() - 127)).unsqueeze(-1)).reshape(*codes.shape[:-1], -1)
+    return torch.ldexp(x, scales.int().unsqueeze(-1) - 127).reshape(*codes.shape[:-1], -1)
 
 
 def _exact_sequence(pool, which, seq, length):
