@@ -51,7 +51,7 @@ enum {
 };
 
 /* bits of the device status word */
-enum { AIF_STATUS_BAD_ID = 1u, AIF_STATUS_TIMEOUT = 2u };
+enum { AIF_STATUS_BAD_ID = 1u, AIF_STATUS_TIMEOUT = 2u, AIF_STATUS_FULL = 4u /* sequence cache: no page left, or a sequence at its longest */ };
 
 enum { AIF_F32 = 0, AIF_BF16 = 1 };
 enum { AIF_BUCKET_MOD = 0, AIF_BUCKET_HASH = 1 };
@@ -345,6 +345,145 @@ int aif_gather_sidecars(aif_ctx *ctx, const int32_t *ids, int64_t n, void *bea_w
 /* Copies the user-side BEA vectors V [n_bridge x d] (storage type) of a state to V_out (device), ordered after the
  * state's user-side call.  AIF_ERR_ARG when the BEA block is off. */
 int aif_user_state_export_bea(aif_ctx *ctx, const aif_user_state *state, void *V_out, aif_stream stream);
+
+/* ---- 4-bit microscaled matrices -------------------------------------------------------------------------------
+ * Dense layers of the item tower and of the scoring model in four bits: weights quantised once, activations per call.  (The
+ * paper leaves the numeric precision of its layers open.)  A matrix [rows x cols], cols a multiple of 32, is held as
+ *   codes   uint8 [rows x cols / 2], row-major, 16-byte aligned: sign, two exponent bits and one mantissa bit (0, .5, 1, 1.5, 2, 3,
+ *           4, 6), two to a byte, the first column in the low half;
+ *   scales  one byte b per 32 consecutive columns of a row, for 2^(b - 127); b = 255 makes every value of the block NaN.  The bytes lie in tiles of
+ *           128 rows x 4 blocks, 512 bytes each, the tiles of 128 rows one after the other (T = ceil(cols / 128) of them): byte (row, block)
+ *           at (row / 128 * T + block / 4) * 512 + row % 32 * 16 + row % 128 / 32 * 4 + block % 4.  16-byte aligned; bytes of rows and
+ *           blocks that only fill up a tile are written by aif_mx4_quantize and have to be kept (any but 255 serves).
+ * These calls need no context.  They run on the device that is current, which has to be the one of their pointers and stream. */
+
+/* Bytes of the scales of a [rows x cols] matrix; AIF_ERR_SHAPE where there is no such matrix. */
+int64_t aif_mx4_scale_bytes(int64_t rows, int32_t cols);
+
+/* x [rows x cols] (dtype AIF_F32 or AIF_BF16, x_stride >= cols elements from row to row, aligned to its elements; rows that begin on 16 bytes are
+ * read faster) to four bits.  A block whose largest magnitude is M has the scale 2^max(floor(log2 M) - 2, -127); a code is the nearest
+ * to x / scale, ties to the one with a zero mantissa bit, never beyond 6.  A block with an infinity or NaN gets the scale byte 255. */
+int aif_mx4_quantize(const void *x, int32_t dtype, int64_t rows, int32_t cols, int64_t x_stride, uint8_t *codes, uint8_t *scales, aif_stream stream);
+
+/* The values that codes and scales stand for, rounded to dtype (exact for the scales that aif_mx4_quantize gives). */
+int aif_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t rows, int32_t cols, void *out, int32_t dtype, int64_t out_stride,
+                       aif_stream stream);
+
+/* Bytes of the workspace of aif_mx4_linear for m rows of k columns that are not quantised yet. */
+int64_t aif_mx4_workspace_bytes(int64_t m, int32_t k);
+
+/* out [m x n] = act(x w^T + bias) for x [m x k] and w [n x k] in four bits; products and scales are exact, sums fp32, rounded
+ * once to dtype.  x is given either as it is (x, x_stride: it is quantised first, exactly as aif_mx4_quantize does) or quantised. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t dtype;             /* of x and out */
+    int64_t m;                 /* rows; 0: nothing is done */
+    int32_t n, k;              /* k a multiple of 32 */
+    const void *x;             /* [m x k], or NULL: the quantised form is given */
+    int64_t x_stride;
+    const uint8_t *x_codes, *x_scales;
+    const uint8_t *w_codes, *w_scales;
+    const float *bias;         /* [n] or NULL */
+    void *out;                 /* [m x n]; may not overlap any input */
+    int64_t out_stride;        /* elements, >= n */
+    void *workspace;           /* with x: aif_mx4_workspace_bytes(m, k) bytes, 16-byte aligned, not shared with a call that may run at the same time */
+    int64_t workspace_bytes;
+    uint32_t *status;          /* device status word (AIF_STATUS_TIMEOUT), or NULL */
+    int32_t relu;              /* 1: act(y) = max(y, 0) */
+    int32_t pad_;
+} aif_mx4_product;
+int aif_mx4_linear(const aif_mx4_product *p, aif_stream stream);
+
+/* ---- behaviour sequences in a cache of 4-bit pages ------------------------------------------------------------
+ * The projected behaviour sequences of many users kept on the GPU between requests (Section 3.3's pre-cache), at 17/32 bytes per value: rows are quantised
+ * as by aif_mx4_quantize when they are appended.  A cache is a set of buffers that the caller owns (device memory of the current
+ * device); every call is ordered on its stream, needs nothing of the host between its launches and can be captured into a graph.  The caller orders calls
+ * that change a cache against all others on it.
+ *
+ * Sequence s has lengths[s] rows; row i of it lies in page table[s][i / page_rows] at i % page_rows.  A page may belong to several
+ * sequences (aif_cache4_fork): refs counts the table entries that name it.  Pages without any stand in free_pages[0 .. n_free), are
+ * handed out from its end, and return to it in the opposite order, so that the same calls on the same cache give the same pages.
+ * What only the GPU can see sets a bit in *status.  It leaves the entry of the call undone: AIF_STATUS_BAD_ID for a sequence outside the cache or one
+ * listed twice (the first stands), AIF_STATUS_FULL where pages or a sequence's table have no room.  It leaves the whole call undone: AIF_STATUS_BAD_ID
+ * for offsets that descend or leave the rows given. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t d;                 /* width of a head: a multiple of 32, <= 256 */
+    int32_t heads;             /* heads of keys and values, 1..64 */
+    int32_t shared;            /* 1: the values are the keys, as in the target attention of aif_score; v_* are NULL */
+    int32_t page_rows;         /* rows of a page: a power of two, 16..1024 */
+    int32_t n_pages;
+    int32_t n_seqs;            /* sequences */
+    int32_t max_pages;         /* pages that a sequence can have; n_seqs * max_pages < 2^31, max_pages * page_rows <= 2^30 */
+    uint8_t *k_codes, *k_scales;   /* [n_pages][heads][page_rows][d / 2] and [..][d / 32]: codes two to a byte, scale bytes; 16-byte aligned */
+    uint8_t *v_codes, *v_scales;
+    int32_t *table;            /* [n_seqs][max_pages]; -1 behind a sequence's last page */
+    int32_t *lengths;          /* [n_seqs] */
+    int32_t *refs;             /* [n_pages] */
+    int32_t *free_pages;       /* [n_pages] */
+    int32_t *n_free;           /* [1] */
+    int32_t *scratch;          /* [aif_cache4_scratch_ints], initialised by aif_cache4_reset */
+    uint32_t *status;          /* [1] */
+} aif_cache4;
+
+int64_t aif_cache4_scratch_ints(const aif_cache4 *c);
+
+/* An empty cache: every page free (page 0 is handed out first), every length 0, the status word 0. */
+int aif_cache4_reset(const aif_cache4 *c, aif_stream stream);
+
+/* Appends rows offsets[i] .. offsets[i + 1] of k (and v) to sequence seq_ids[i], for i < n.  seq_ids: device int32 [n], distinct; offsets: device
+ * int64 [n + 1], ascending, within [0, rows].  k, v: device [rows x heads x d] of dtype, `stride` elements from row to row, aligned to their elements; v
+ * NULL iff the cache is shared.  A last page that is only partly filled and belongs to other sequences too is copied first (the
+ * others keep theirs).  Entries are served in their order; from the first one on that finds too few free pages, entries that need any are left undone. */
+int aif_cache4_append(const aif_cache4 *c, int32_t n, const int32_t *seq_ids, const int64_t *offsets, const void *k, const void *v, int32_t dtype,
+                      int64_t rows, int64_t stride, aif_stream stream);
+
+/* Sequence dst[i] becomes sequence src[i], on the same pages (fork) or on pages of its own with the same contents (copy); what
+ * it was before is freed first.  A snapshot for the requests in flight while rows are appended to src (the consistency that Section 3.4 asks
+ * for).  src, dst: device int32 [n]; dst distinct, and no src among them (AIF_STATUS_BAD_ID, the entry is left undone). */
+int aif_cache4_fork(const aif_cache4 *c, int32_t n, const int32_t *src, const int32_t *dst, aif_stream stream);
+int aif_cache4_copy(const aif_cache4 *c, int32_t n, const int32_t *src, const int32_t *dst, aif_stream stream);
+
+/* Empties the sequences; pages that nobody else has return to the free ones. */
+int aif_cache4_free(const aif_cache4 *c, int32_t n, const int32_t *seq_ids, aif_stream stream);
+
+/* All sequences of c into the cache `into` (of the same d, heads, shared, page_rows, n_seqs and max_pages, any n_pages; no buffer in common), whose former contents
+ * are dropped: the pages in use take the pages 0, 1, ... in their order, shared ones stay shared.  c is left as it is.  With too
+ * few pages `into` is left empty, with AIF_STATUS_FULL in its status. */
+int aif_cache4_compact(const aif_cache4 *c, const aif_cache4 *into, aif_stream stream);
+
+/* The first offsets[i + 1] - offsets[i] rows of sequence seq_ids[i], as values, to rows offsets[i] .. of k_out (and v_out): e.g. the projected
+ * sequence that aif_user_precompute takes.  Rows behind a sequence's end, or of a bad id, are zero, with AIF_STATUS_BAD_ID.  A sequence may be listed
+ * more than once.  Rows of the outputs that no entry names stay as they are.  v_out: NULL iff shared. */
+int aif_cache4_read(const aif_cache4 *c, int32_t n, const int32_t *seq_ids, const int64_t *offsets, void *k_out, void *v_out, int32_t dtype,
+                    int64_t rows, int64_t stride, aif_stream stream);
+
+/* Attention of query rows over the sequences of a cache (Section 4.2's target attention, eq. 3's profile attention):
+ *   out = sum_j p_j v_j,   p = softmax_j(scale q k_j)   over the rows j of the sequence that are visible:
+ * all of them, or with window > 0 the last `window` rows and the first `sinks` ones.  Query head h attends to head h / (n_heads / heads) of the cache. A
+ * sequence without rows gives zero rows; one with a bad id, length or page gives NaN and AIF_STATUS_BAD_ID. */
+typedef struct {
+    uint32_t struct_size;
+    int32_t dtype;             /* of q and out */
+    int32_t n_heads;           /* a multiple of the cache's heads, <= 64 times them */
+    int32_t n;                 /* sequences of the call; 0: nothing is done */
+    const int32_t *seq_ids;    /* device [n], or NULL: sequences 0 .. n - 1.  May repeat */
+    const int64_t *offsets;    /* device [n + 1]: rows offsets[i] .. offsets[i + 1] of q belong to sequence i; NULL: row i (rows == n) */
+    int64_t rows;              /* rows of q and out; those that no sequence names are neither read nor written */
+    const void *q;             /* [rows x n_heads x d], q_stride elements from row to row; 16-byte aligned rows */
+    void *out;                 /* likewise; may not overlap q */
+    int64_t q_stride, out_stride;
+    float scale;               /* 0: 1 / sqrt(d) */
+    int32_t window, sinks;     /* window 0: all rows are visible, sinks is not used */
+    int32_t pad_;
+    void *workspace;           /* aif_cache4_attention_workspace bytes, 16-byte aligned; not shared with a call that may run at the same time */
+    int64_t workspace_bytes;
+} aif_cache4_query;
+int64_t aif_cache4_attention_workspace(const aif_cache4 *c, const aif_cache4_query *q);
+int aif_cache4_attention(const aif_cache4 *c, const aif_cache4_query *q, aif_stream stream);
+
+/* Reads and clears the cache's status word (synchronises `stream`).  bits: host. */
+int aif_cache4_poll(const aif_cache4 *c, uint32_t *bits, aif_stream stream);
 
 /* Reads and clears the device status word (synchronises the device).  bits: host. */
 int aif_poll_status(aif_ctx *ctx, uint32_t *bits);

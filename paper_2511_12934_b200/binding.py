@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from array import array
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 import torch
@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libaif.so")
 
 OK = 0
 ERR_ARG, ERR_SHAPE, ERR_OOM, ERR_CUDA, ERR_VERSION, ERR_NOT_READY, ERR_BAD_ID, ERR_TIMEOUT = -1, -2, -3, -4, -5, -6, -7, -8
-STATUS_BAD_ID, STATUS_TIMEOUT = 1, 2
+STATUS_BAD_ID, STATUS_TIMEOUT, STATUS_FULL = 1, 2, 4
 F32, BF16 = 0, 1
 BUCKET_MOD, BUCKET_HASH = 0, 1
 NORM_NONE, NORM_MEAN = 0, 1
@@ -79,6 +79,33 @@ class aif_stats(C.Structure):
     ]
 
 
+class aif_mx4_product(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_int32), ("m", C.c_int64), ("n", C.c_int32), ("k", C.c_int32), ("x", C.c_void_p),
+        ("x_stride", C.c_int64), ("x_codes", C.c_void_p), ("x_scales", C.c_void_p), ("w_codes", C.c_void_p), ("w_scales", C.c_void_p),
+        ("bias", C.c_void_p), ("out", C.c_void_p), ("out_stride", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
+        ("status", C.c_void_p), ("relu", C.c_int32), ("pad_", C.c_int32),
+    ]
+
+
+class aif_cache4(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("d", C.c_int32), ("heads", C.c_int32), ("shared", C.c_int32), ("page_rows", C.c_int32),
+        ("n_pages", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("k_codes", C.c_void_p), ("k_scales", C.c_void_p),
+        ("v_codes", C.c_void_p), ("v_scales", C.c_void_p), ("table", C.c_void_p), ("lengths", C.c_void_p), ("refs", C.c_void_p),
+        ("free_pages", C.c_void_p), ("n_free", C.c_void_p), ("scratch", C.c_void_p), ("status", C.c_void_p),
+    ]
+
+
+class aif_cache4_query(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_int32), ("n_heads", C.c_int32), ("n", C.c_int32), ("seq_ids", C.c_void_p),
+        ("offsets", C.c_void_p), ("rows", C.c_int64), ("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_int64), ("out_stride", C.c_int64),
+        ("scale", C.c_float), ("window", C.c_int32), ("sinks", C.c_int32), ("pad_", C.c_int32), ("workspace", C.c_void_p),
+        ("workspace_bytes", C.c_int64),
+    ]
+
+
 # every symbol include/aif.h declares
 EXPORTS = [
     "aif_input_width", "aif_mix64", "aif_category", "aif_create", "aif_destroy", "aif_load_weights", "aif_item_nearline_refresh",
@@ -86,6 +113,9 @@ EXPORTS = [
     "aif_user_precompute", "aif_user_release", "aif_user_request_key", "aif_user_state_export", "aif_user_state_export_bea", "aif_score",
     "aif_score_batch", "aif_score_host", "aif_score_batch_host", "aif_score_noalloc", "aif_gather_rows", "aif_gather_sidecars", "aif_poll_status", "aif_get_stats",
     "aif_set_kernel_timing", "aif_get_kernel_timing", "aif_kernel_launches", "aif_selftest_bounded_wait", "aif_strerror", "aif_last_error",
+    "aif_mx4_scale_bytes", "aif_mx4_quantize", "aif_mx4_dequantize", "aif_mx4_workspace_bytes", "aif_mx4_linear",
+    "aif_cache4_scratch_ints", "aif_cache4_reset", "aif_cache4_append", "aif_cache4_fork", "aif_cache4_copy", "aif_cache4_free", "aif_cache4_compact",
+    "aif_cache4_read", "aif_cache4_attention_workspace", "aif_cache4_attention", "aif_cache4_poll",
 ]
 
 _lib = None
@@ -130,6 +160,23 @@ def load_library(path: Optional[str] = None):
     lib.aif_selftest_bounded_wait.argtypes = [vp, i64, vp]
     lib.aif_strerror.argtypes, lib.aif_strerror.restype = [C.c_int], C.c_char_p
     lib.aif_last_error.argtypes, lib.aif_last_error.restype = [], C.c_char_p
+    c4, q4 = C.POINTER(aif_cache4), C.POINTER(aif_cache4_query)
+    lib.aif_mx4_scale_bytes.argtypes, lib.aif_mx4_scale_bytes.restype = [i64, i32], i64
+    lib.aif_mx4_workspace_bytes.argtypes, lib.aif_mx4_workspace_bytes.restype = [i64, i32], i64
+    lib.aif_mx4_quantize.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp]
+    lib.aif_mx4_dequantize.argtypes = [vp, vp, i64, i32, vp, i32, i64, vp]
+    lib.aif_mx4_linear.argtypes = [C.POINTER(aif_mx4_product), vp]
+    lib.aif_cache4_scratch_ints.argtypes, lib.aif_cache4_scratch_ints.restype = [c4], i64
+    lib.aif_cache4_reset.argtypes = [c4, vp]
+    lib.aif_cache4_append.argtypes = [c4, i32, vp, vp, vp, vp, i32, i64, i64, vp]
+    lib.aif_cache4_fork.argtypes = [c4, i32, vp, vp, vp]
+    lib.aif_cache4_copy.argtypes = [c4, i32, vp, vp, vp]
+    lib.aif_cache4_free.argtypes = [c4, i32, vp, vp]
+    lib.aif_cache4_compact.argtypes = [c4, c4, vp]
+    lib.aif_cache4_read.argtypes = [c4, i32, vp, vp, vp, vp, i32, i64, i64, vp]
+    lib.aif_cache4_attention_workspace.argtypes, lib.aif_cache4_attention_workspace.restype = [c4, q4], i64
+    lib.aif_cache4_attention.argtypes = [c4, q4, vp]
+    lib.aif_cache4_poll.argtypes = [c4, C.POINTER(C.c_uint32), vp]
     if path is None:
         _lib = lib
     return lib
@@ -389,3 +436,300 @@ class Aif:
         s = aif_stats()
         _check(self.lib.aif_get_stats(self.h, C.byref(s)), "aif_get_stats")
         return s
+
+
+# -- 4-bit matrices and the 4-bit sequence cache ------------------------------------------------------
+# These need no context: they run on the device of their tensors, on its current stream or the one given.  Workspaces come
+# from torch's allocator on that stream, per call, so calls on several streams and captured graphs never share one.
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+class _Launch:
+    """The device of a call's tensors made current, and the raw stream; `alloc` allocates for use on that stream."""
+
+    def __init__(self, device: torch.device, stream):
+        if stream is not None and stream.device != device:
+            raise ValueError(f"stream on {stream.device}, tensors on {device}")
+        self.device, self.stream = device, stream
+        self.other = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+        self.raw = _current_raw_stream(self.device.index) if self.stream is None else self.stream.cuda_stream
+        return self
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
+
+    def alloc(self, n: int) -> torch.Tensor:
+        if self.stream is None:
+            return torch.empty(n, dtype=torch.uint8, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(n, dtype=torch.uint8, device=self.device)
+
+
+def _tensor(t, name: str, dtype, shape, device: torch.device, dense: bool = True) -> torch.Tensor:
+    """`t` checked: on `device`, of dtype and shape (None: any size), contiguous (dense) or at least with its rows in one piece."""
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise ValueError(f"{name}: a tensor on {device} is needed")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: {dtype} is needed, not {t.dtype}")
+    if t.dim() != len(shape) or any(w is not None and w != g for w, g in zip(shape, t.shape)):
+        raise ValueError(f"{name}: shape {tuple(shape)} is needed, not {tuple(t.shape)}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous")
+    return t
+
+
+def _rows(t: torch.Tensor, name: str, heads: int, d: int, device: torch.device, dtype=None) -> int:
+    """[rows x heads x d] (or [rows x d] with one head), fp32 or bf16, a row in one piece: the elements from row to row."""
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise ValueError(f"{name}: a tensor on {device} is needed")
+    if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name}: {dtype or 'float32 or bfloat16'} is needed, not {t.dtype}")
+    if tuple(t.shape[1:]) != (heads, d) and not (heads == 1 and tuple(t.shape[1:]) == (d,)):
+        raise ValueError(f"{name}: shape [rows, {heads}, {d}] is needed, not {tuple(t.shape)}")
+    if t.stride(-1) != 1 or (t.dim() == 3 and heads > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}: the heads of a row have to lie one after the other")
+    return t.stride(0) if t.shape[0] > 1 else heads * d
+
+
+def _cuda_device(t, name: str) -> torch.device:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name}: a CUDA tensor is needed")
+    return t.device
+
+
+class Mx4(NamedTuple):
+    """A matrix [rows x cols] in 4-bit microscaled form: codes uint8 [rows, cols / 2] and scale bytes (see include/aif.h)."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    @property
+    def rows(self) -> int:
+        return self.codes.shape[0]
+
+    @property
+    def cols(self) -> int:
+        return 2 * self.codes.shape[1]
+
+
+def _mx4_check(m: Mx4, name: str, device: torch.device) -> Mx4:
+    _tensor(m.codes, name + ".codes", torch.uint8, (None, None), device)
+    n = load_library().aif_mx4_scale_bytes(m.rows, m.cols)
+    if n < 0:
+        _check(n, name)
+    _tensor(m.scales, name + ".scales", torch.uint8, (n,), device)
+    return m
+
+
+def mx4_empty(rows: int, cols: int, device="cuda") -> Mx4:
+    n = load_library().aif_mx4_scale_bytes(rows, cols)
+    if n < 0:
+        _check(n, "mx4_empty")
+    return Mx4(torch.empty(rows, cols // 2, dtype=torch.uint8, device=device), torch.empty(n, dtype=torch.uint8, device=device))
+
+
+def mx4_quantize(x: torch.Tensor, out: Optional[Mx4] = None, stream=None) -> Mx4:
+    """x [rows, cols] (float32 or bfloat16, cols a multiple of 32) in 4 bits; into `out` if given."""
+    device = _cuda_device(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x: a matrix is needed")
+    stride = _rows(x, "x", 1, x.shape[1], device)
+    with _Launch(device, stream) as at:
+        if out is None:
+            with torch.cuda.stream(stream):
+                out = mx4_empty(x.shape[0], x.shape[1], device)
+        elif (out.rows, out.cols) != tuple(x.shape):
+            raise ValueError(f"out: [{x.shape[0]} x {x.shape[1]}] is needed, not [{out.rows} x {out.cols}]")
+        _mx4_check(out, "out", device)
+        _check(load_library().aif_mx4_quantize(x.data_ptr(), _DTYPES[x.dtype], x.shape[0], x.shape[1], stride, out.codes.data_ptr(), out.scales.data_ptr(),
+                                               at.raw), "aif_mx4_quantize")
+    return out
+
+
+def mx4_dequantize(m: Mx4, out: torch.Tensor, stream=None) -> torch.Tensor:
+    """The values of m into out [rows, cols] (float32 or bfloat16)."""
+    device = _cuda_device(out, "out")
+    _mx4_check(m, "m", device)
+    stride = _rows(out, "out", 1, m.cols, device)
+    if out.shape[0] != m.rows:
+        raise ValueError(f"out: {m.rows} rows are needed, not {out.shape[0]}")
+    with _Launch(device, stream) as at:
+        _check(load_library().aif_mx4_dequantize(m.codes.data_ptr(), m.scales.data_ptr(), m.rows, m.cols, out.data_ptr(), _DTYPES[out.dtype], stride, at.raw),
+               "aif_mx4_dequantize")
+    return out
+
+
+def mx4_linear(x, w: Mx4, out: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False, status: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """out [m, n] = act(x w^T + bias): x [m, k] as a tensor of out's type (quantised on the way) or as an Mx4, w [n, k] an Mx4, bias float32 [n];
+    status: a uint32-sized int32 tensor that takes AIF_STATUS_TIMEOUT."""
+    device = _cuda_device(out, "out")
+    _mx4_check(w, "w", device)
+    m, n, k = out.shape[0], w.rows, w.cols
+    p = aif_mx4_product()
+    p.struct_size, p.m, p.n, p.k, p.relu = C.sizeof(aif_mx4_product), m, n, k, 1 if relu else 0
+    p.out_stride = _rows(out, "out", 1, n, device)
+    p.dtype, p.out = _DTYPES[out.dtype], out.data_ptr()
+    p.w_codes, p.w_scales = w.codes.data_ptr(), w.scales.data_ptr()
+    if bias is not None:
+        p.bias = _tensor(bias, "bias", torch.float32, (n,), device).data_ptr()
+    if status is not None:
+        p.status = _tensor(status, "status", torch.int32, (1,), device).data_ptr()
+    rows = x.rows if isinstance(x, Mx4) else x.shape[0]
+    if rows != m:
+        raise ValueError(f"x: {m} rows are needed, not {rows}")
+    with _Launch(device, stream) as at:
+        keep = None
+        if isinstance(x, Mx4):
+            if x.cols != k:
+                raise ValueError(f"x: {k} columns are needed, not {x.cols}")
+            _mx4_check(x, "x", device)
+            p.x_codes, p.x_scales = x.codes.data_ptr(), x.scales.data_ptr()
+        else:
+            p.x_stride = _rows(x, "x", 1, k, device, out.dtype)
+            p.x = x.data_ptr()
+            keep = at.alloc(max(16, load_library().aif_mx4_workspace_bytes(m, k)))
+            p.workspace, p.workspace_bytes = keep.data_ptr(), keep.numel()
+        _check(load_library().aif_mx4_linear(C.byref(p), at.raw), "aif_mx4_linear")
+    return out
+
+
+class Cache4:
+    """Behaviour sequences in 4-bit pages (see include/aif.h).  The buffers are attributes: k_codes [n_pages, heads, page_rows, d / 2] and k_scales [.., d / 32]
+    (v_codes, v_scales unless the values are the keys), table [n_seqs, max_pages], lengths, refs, free_pages, n_free, status."""
+
+    def __init__(self, *, d: int, n_pages: int, page_rows: int, n_seqs: int, max_pages: int, heads: int = 1, shared: bool = True, device="cuda", stream=None):
+        if not torch.cuda.is_available():
+            raise RuntimeError("the sequence cache needs a CUDA device; there is no CPU path")
+        device = torch.device(device)
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+        self.d, self.heads, self.page_rows, self.shared = d, heads, page_rows, bool(shared)
+        self.n_pages, self.n_seqs, self.max_pages = n_pages, n_seqs, max_pages
+        self.lib = load_library()
+        c = aif_cache4(C.sizeof(aif_cache4), d, heads, 1 if shared else 0, page_rows, n_pages, n_seqs, max_pages)
+        n_scratch = self.lib.aif_cache4_scratch_ints(C.byref(c))
+        if n_scratch < 0:
+            _check(n_scratch, "Cache4")
+        if d < 32 or d % 32 or page_rows < 1 or heads < 1 or max_pages < 1:
+            _check(ERR_SHAPE, "Cache4")
+        with _Launch(self.device, stream), torch.cuda.stream(stream):
+            def ints(*shape):
+                return torch.empty(*shape, dtype=torch.int32, device=self.device)
+
+            def codes():
+                return (torch.empty(n_pages, heads, page_rows, d // 2, dtype=torch.uint8, device=self.device),
+                        torch.empty(n_pages, heads, page_rows, d // 32, dtype=torch.uint8, device=self.device))
+
+            self.k_codes, self.k_scales = codes()
+            self.v_codes, self.v_scales = (None, None) if shared else codes()
+            self.table, self.lengths, self.refs, self.free_pages = ints(n_seqs, max_pages), ints(n_seqs), ints(n_pages), ints(n_pages)
+            self.n_free, self.status, self._scratch = ints(1), ints(1), ints(n_scratch)
+        for name in ("k_codes", "k_scales", "v_codes", "v_scales", "table", "lengths", "refs", "free_pages", "n_free", "status"):
+            t = getattr(self, name)
+            setattr(c, name, None if t is None else t.data_ptr())
+        c.scratch = self._scratch.data_ptr()
+        self._c = c
+        self.reset(stream=stream)
+
+    def _ids(self, t: torch.Tensor, name: str) -> int:
+        return _tensor(t, name, torch.int32, (None,), self.device).shape[0]
+
+    def _rows(self, offsets, n: int, k, v, k_name: str, v_name: str) -> int:
+        _tensor(offsets, "offsets", torch.int64, (n + 1,), self.device)
+        stride = _rows(k, k_name, self.heads, self.d, self.device)
+        if (v is None) != self.shared:
+            raise ValueError(f"{v_name}: {'this cache has no values of its own' if self.shared else 'is needed'}")
+        if v is not None:
+            if _rows(v, v_name, self.heads, self.d, self.device, k.dtype) != stride or v.shape[0] != k.shape[0]:
+                raise ValueError(f"{v_name}: the rows and the stride of {k_name} are needed")
+        return stride
+
+    def reset(self, stream=None):
+        """Empties the cache."""
+        with _Launch(self.device, stream) as at:
+            _check(self.lib.aif_cache4_reset(C.byref(self._c), at.raw), "aif_cache4_reset")
+
+    def append(self, seq_ids: torch.Tensor, offsets: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor] = None, stream=None):
+        """Rows offsets[i] .. offsets[i + 1] of k (and v) to the end of sequence seq_ids[i]."""
+        n = self._ids(seq_ids, "seq_ids")
+        stride = self._rows(offsets, n, k, v, "k", "v")
+        with _Launch(self.device, stream) as at:
+            _check(self.lib.aif_cache4_append(C.byref(self._c), n, seq_ids.data_ptr(), offsets.data_ptr(), k.data_ptr(), None if v is None else v.data_ptr(),
+                                              _DTYPES[k.dtype], k.shape[0], stride, at.raw), "aif_cache4_append")
+
+    def read(self, seq_ids: torch.Tensor, offsets: torch.Tensor, k_out: torch.Tensor, v_out: Optional[torch.Tensor] = None, stream=None):
+        """The first offsets[i + 1] - offsets[i] rows of sequence seq_ids[i] as values, to rows offsets[i] .. of k_out (and v_out)."""
+        n = self._ids(seq_ids, "seq_ids")
+        stride = self._rows(offsets, n, k_out, v_out, "k_out", "v_out")
+        with _Launch(self.device, stream) as at:
+            _check(self.lib.aif_cache4_read(C.byref(self._c), n, seq_ids.data_ptr(), offsets.data_ptr(), k_out.data_ptr(),
+                                            None if v_out is None else v_out.data_ptr(), _DTYPES[k_out.dtype], k_out.shape[0], stride, at.raw), "aif_cache4_read")
+
+    def _share(self, call, src: torch.Tensor, dst: torch.Tensor, stream):
+        n = self._ids(src, "src")
+        _tensor(dst, "dst", torch.int32, (n,), self.device)
+        with _Launch(self.device, stream) as at:
+            _check(call(C.byref(self._c), n, src.data_ptr(), dst.data_ptr(), at.raw), call.__name__)
+
+    def fork(self, src: torch.Tensor, dst: torch.Tensor, stream=None):
+        """Sequence dst[i] becomes a snapshot of src[i] on the same pages."""
+        self._share(self.lib.aif_cache4_fork, src, dst, stream)
+
+    def copy(self, src: torch.Tensor, dst: torch.Tensor, stream=None):
+        """Sequence dst[i] becomes a copy of src[i] on pages of its own."""
+        self._share(self.lib.aif_cache4_copy, src, dst, stream)
+
+    def free(self, seq_ids: torch.Tensor, stream=None):
+        n = self._ids(seq_ids, "seq_ids")
+        with _Launch(self.device, stream) as at:
+            _check(self.lib.aif_cache4_free(C.byref(self._c), n, seq_ids.data_ptr(), at.raw), "aif_cache4_free")
+
+    def compact(self, into: "Cache4", stream=None):
+        """All sequences into the cache `into`, pages in use first and in their order."""
+        if into.device != self.device:
+            raise ValueError(f"into: a cache on {self.device} is needed")
+        with _Launch(self.device, stream) as at:
+            _check(self.lib.aif_cache4_compact(C.byref(self._c), C.byref(into._c), at.raw), "aif_cache4_compact")
+
+    def attention(self, q: torch.Tensor, out: torch.Tensor, seq_ids: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None, scale: float = 0.0,
+                  window: int = 0, sinks: int = 0, stream=None) -> torch.Tensor:
+        """out = softmax(scale q K^T) V over the visible rows of the sequences: q, out [rows, n_heads, d] or [rows, d]; rows offsets[i] .. offsets[i + 1]
+        belong to sequence seq_ids[i] (default: i), without offsets row i.  scale 0: 1 / sqrt(d).  window > 0: the last `window` rows and the first `sinks`."""
+        heads = q.shape[1] if q.dim() == 3 else 1
+        if heads < 1 or heads % self.heads:
+            raise ValueError(f"q: a multiple of {self.heads} heads is needed, not {heads}")
+        a = aif_cache4_query()
+        a.struct_size, a.n_heads, a.rows = C.sizeof(aif_cache4_query), heads, q.shape[0]
+        a.q_stride = _rows(q, "q", heads, self.d, self.device)
+        a.dtype, a.q = _DTYPES[q.dtype], q.data_ptr()
+        a.out_stride = _rows(out, "out", heads, self.d, self.device, q.dtype)
+        if out.shape[0] != q.shape[0]:
+            raise ValueError(f"out: {q.shape[0]} rows are needed, not {out.shape[0]}")
+        a.out = out.data_ptr()
+        a.n = q.shape[0]
+        if seq_ids is not None:
+            a.n, a.seq_ids = self._ids(seq_ids, "seq_ids"), seq_ids.data_ptr()
+        elif offsets is not None:
+            a.n = max(0, offsets.numel() - 1)
+        if offsets is not None:
+            a.offsets = _tensor(offsets, "offsets", torch.int64, (a.n + 1,), self.device).data_ptr()
+        a.scale, a.window, a.sinks = scale, window, sinks
+        n_bytes = self.lib.aif_cache4_attention_workspace(C.byref(self._c), C.byref(a))
+        if n_bytes < 0:
+            _check(n_bytes, "aif_cache4_attention")
+        with _Launch(self.device, stream) as at:
+            keep = at.alloc(max(16, n_bytes))
+            a.workspace, a.workspace_bytes = keep.data_ptr(), keep.numel()
+            _check(self.lib.aif_cache4_attention(C.byref(self._c), C.byref(a), at.raw), "aif_cache4_attention")
+        return out
+
+    def poll_status(self, stream=None) -> int:
+        """Status bits since the last call (STATUS_BAD_ID, STATUS_FULL, STATUS_TIMEOUT); waits for the stream."""
+        bits = C.c_uint32()
+        with _Launch(self.device, stream) as at:
+            _check(self.lib.aif_cache4_poll(C.byref(self._c), C.byref(bits), at.raw), "aif_cache4_poll")
+        return int(bits.value)

@@ -1,0 +1,134 @@
+// 4-bit microscaled values: E2M1 codes (sign, two exponent bits, one mantissa bit: 0, .5, 1, 1.5, 2, 3, 4, 6) in blocks of 32
+// that share a power of two, kept as a byte b = exponent + 127 (E8M0).  Two codes to a byte, the first in the low half.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace aif {
+namespace {
+
+constexpr int kMxBlock = 32;      // elements that share a scale
+constexpr uint32_t kMxNan = 255;  // scale byte of a block that holds an infinity or NaN: every value of it is NaN
+
+// Scale byte of a block whose largest magnitude has these bits (fp32, sign off): the exponent of the largest value less the two of
+// the largest code, never below 2^-127.  A plain difference of exponent fields, subnormal blocks included.
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t top_bits)
+{
+    const uint32_t field = top_bits >> 23;
+    return field == 255u ? kMxNan : field > 2u ? field - 2u : 0u;
+}
+// 2^(127 - byte) for the byte of a block without infinities; its products with the block's elements are exact.
+__device__ __forceinline__ float mx_inverse_scale(uint32_t byte) { return byte == kMxNan ? 0.f : __uint_as_float((254u - byte) << 23); }
+// 2^(byte - 127); NaN for kMxNan.
+__device__ __forceinline__ float mx_scale(uint32_t byte)
+{
+    return __uint_as_float(byte == 0u ? 0x00400000u : byte == kMxNan ? 0x7fffffffu : byte << 23);
+}
+
+// Eight values -> eight codes, to nearest (ties to the code with a zero mantissa bit), saturating at +-6.
+__device__ __forceinline__ uint32_t mx_encode8(const float (&v)[8])
+{
+    uint32_t w;
+    asm("{\n"
+        ".reg .b8 a, b, c, d;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n"
+        "mov.b32 %0, {a, b, c, d};\n"
+        "}\n"
+        : "=r"(w)
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return w;
+}
+// Eight codes -> four pairs of fp16 (exact, unscaled): o[i] = values 2 i and 2 i + 1.
+__device__ __forceinline__ void mx_decode8_f16(uint32_t w, uint32_t (&o)[4])
+{
+    asm("{\n"
+        ".reg .b8 a, b, c, d;\n"
+        "mov.b32 {a, b, c, d}, %4;\n"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n"
+        "cvt.rn.f16x2.e2m1x2 %3, d;\n"
+        "}\n"
+        : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
+        : "r"(w));
+}
+__device__ __forceinline__ float2 half2_to_float2(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2 *>(&h)); }
+
+// Eight consecutive elements of storage type T as fp32.  ALIGNED: the address is a multiple of 16 bytes.
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void load8(const T *p, float (&v)[8])
+{
+    if constexpr (!ALIGNED) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)p[i];
+    } else if constexpr (sizeof(T) == 2) {
+        const uint4 r = __ldg(reinterpret_cast<const uint4 *>(p));
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+        const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    }
+}
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ void store8(T *p, const float (&v)[8])
+{
+    if constexpr (!ALIGNED) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = (T)v[i];
+    } else if constexpr (sizeof(T) == 2) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+}
+
+// Four neighbouring lanes (4 i .. 4 i + 3, converged) quantise the 32 elements of one block, eight each: the lane's codes, and the block's scale byte.
+__device__ __forceinline__ uint32_t mx_quantise_quad(const float (&x)[8], uint32_t &byte)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);   // as integers: NaN stays the largest
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    byte = mx_scale_byte(top);
+    const float inv = mx_inverse_scale(byte);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = byte == kMxNan ? 0.f : x[i] * inv;
+    return mx_encode8(y);
+}
+// The values of eight codes of a block with this scale.
+__device__ __forceinline__ void mx_values8(uint32_t codes, float scale, float (&v)[8])
+{
+    uint32_t h[4];
+    mx_decode8_f16(codes, h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = half2_to_float2(h[i]);
+        v[2 * i] = f.x * scale, v[2 * i + 1] = f.y * scale;
+    }
+}
+
+// Scale bytes of a matrix lie in tiles of 128 rows x 4 blocks, 512 bytes each, the tiles of a band of 128 rows one after the other:
+// byte (row, block) at (row / 128 * tiles + block / 4) * 512 + row % 32 * 16 + row % 128 / 32 * 4 + block % 4, which is the order in
+// which the block-scaled products read 32 rows x 16 bytes into tensor memory.
+__host__ __device__ __forceinline__ int mx_scale_tiles(int cols) { return (cols + 4 * kMxBlock - 1) / (4 * kMxBlock); }
+__device__ __forceinline__ int mx_scale_at(int row_in_band, int block_in_tile) { return (row_in_band & 31) * 16 + (row_in_band >> 5) * 4 + block_in_tile; }
+
+}  // namespace
+}  // namespace aif

@@ -1,0 +1,328 @@
+// Product of two matrices of 4-bit microscaled values on the tensor cores (sm_100a, block-scaled tcgen05 products):
+//   out[i][j] = act(sum_k a_ik w_jk + bias_j),  a [m x k], w [n x k], blocks of 32 along k with a scale each.
+// Products of codes and their scales are exact; sums, bias and activation are fp32, rounded once to the type of `out`.
+//
+// One CTA per SM walks over tiles of 128 rows x 128 columns, columns fastest, so that the rows of a tile come from HBM once and from
+// L2 for the other columns.  Warps: 0 streams stages of 256 k (128 bytes of codes per row by TMA, the scale tiles by bulk copies);
+// 1 copies a stage's scales to tensor memory and issues its four products of 64 k; 4-7 take a finished accumulator out of tensor memory while the
+// next tile is at work (two accumulators), stage it in shared memory and store whole 128-byte pieces of rows.
+// The scale copies go to tensor-memory columns of their own per stage: a stage is only refilled once its products have completed.
+#include <climits>
+#include <cstdio>
+
+#include "aif_internal.h"
+#include "aif_mx4.cuh"
+#include "aif_tc_ptx.cuh"
+
+namespace aif {
+
+cudaError_t launch_mx4_quantize(const void *x, int dtype, int64_t rows, int cols, int64_t stride, uint8_t *codes, uint8_t *scales, cudaStream_t st);
+
+namespace {
+
+// Instruction descriptor of tcgen05.mma.kind::mxf4: A and B E2M1 (1 at [7,10) and [10,12)), N >> 3 at [17,23), scales E8M0 (bit 23), M >> 4 at
+// [24,29); which pair of the four scale bytes of a column an instruction uses (0 or 2) stands at [4,6) for B and [29,31) for A.
+__host__ __device__ constexpr uint32_t umma_idesc_mxf4(int m, int n, int pair)
+{
+    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 4) << 24) | ((uint32_t)pair << 29) | ((uint32_t)pair << 4);
+}
+__device__ __forceinline__ void umma_mxf4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t a_scale, uint32_t b_scale, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "setp.ne.b32 p, %6, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n"
+        "}\n" ::"r"(d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+        : "memory");
+}
+// 512 bytes (32 rows x 16 bytes) to four tensor-memory columns, the same in every quarter of the lanes.
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc)
+{
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+constexpr int kBM = 128;
+constexpr int kStageK = 256;       // elements of k per stage: 128 bytes of codes, two scale tiles
+constexpr int kTmemScales = 256;   // first of the scale columns, behind the two accumulators (at 0 and 128)
+
+constexpr int kBN = 128;
+
+struct GemmCfg {
+    static constexpr int kABytes = kBM * 128, kBBytes = kBN * 128;
+    static constexpr int kStageBytes = kABytes + kBBytes + 2048;   // + two scale tiles of each operand
+    static constexpr int kStages = 5;
+    static constexpr int kThreads = 256;
+    static constexpr int kOutBytes = 4 * 4096;                     // 32 rows x 128 bytes for each of the four output warps
+    static constexpr size_t kSmem = 1024 + kStages * kStageBytes + kOutBytes + 256;
+};
+
+struct GemmParams {
+    int64_t m;
+    int32_t n, k;
+    const uint8_t *a_scales, *w_scales;
+    const float *bias;
+    int32_t relu;
+    void *out;
+    int64_t out_stride;
+    int32_t wide;        // rows of `out` begin on 16-byte boundaries
+    int32_t n_tiles;     // column tiles
+    int64_t tiles;
+    uint32_t *status;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, const GemmParams p)
+{
+    using C = GemmCfg;
+    constexpr int kS = C::kStages;
+    extern __shared__ unsigned char smem_dyn[];
+    unsigned char *base = reinterpret_cast<unsigned char *>(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
+    unsigned char *smA = base, *smB = smA + kS * C::kABytes, *smSc = smB + kS * C::kBBytes;   // scales: [stage][A 1 KB, W 1 KB]
+    unsigned char *smOut = smSc + kS * 2048;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smOut + C::kOutBytes);
+    uint64_t *full = bars, *empty = bars + kS, *acc_full = bars + 2 * kS, *acc_empty = acc_full + 2;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(acc_empty + 2);
+    volatile uint32_t *abort_flag = tmem_slot + 1;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < kS; ++s) mbar_init(smem_u32(full + s), 1), mbar_init(smem_u32(empty + s), 1);
+        for (int b = 0; b < 2; ++b) mbar_init(smem_u32(acc_full + b), 1), mbar_init(smem_u32(acc_empty + b), 4);
+        *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    grid_dep_wait();
+    grid_dep_launch();
+
+    const int stages = (p.k + kStageK - 1) / kStageK, sc_tiles = mx_scale_tiles(p.k);
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (int64_t tile = blockIdx.x; ok && tile < p.tiles; tile += gridDim.x) {
+                const int64_t band = tile / p.n_tiles;
+                const int n0 = (int)(tile % p.n_tiles) * kBN;
+                const uint8_t *sa = p.a_scales + (size_t)band * sc_tiles * 512;
+                const uint8_t *sw = p.w_scales + (size_t)(n0 / 128) * sc_tiles * 512;
+                for (int j = 0; j < stages; ++j, ++it) {
+                    const int s = (int)(it % kS);
+                    if (!mbar_wait(smem_u32(empty + s), ((it / kS) & 1u) ^ 1u, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t sc = (uint32_t)(min(2, sc_tiles - 2 * j) * 512), bar = smem_u32(full + s);
+                    mbar_expect_tx(bar, (uint32_t)(C::kABytes + C::kBBytes) + 2 * sc);
+                    tma_load_2d(smem_u32(smA + s * C::kABytes), &tmA, bar, j * 128, (int)(band * kBM));
+                    tma_load_2d(smem_u32(smB + s * C::kBBytes), &tmW, bar, j * 128, n0);
+                    bulk_load(smem_u32(smSc + s * 2048), sa + j * 1024, sc, bar);
+                    bulk_load(smem_u32(smSc + s * 2048 + 1024), sw + j * 1024, sc, bar);
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            int t = 0;
+            bool ok = true;
+            for (int64_t tile = blockIdx.x; ok && tile < p.tiles; tile += gridDim.x, ++t) {
+                const int b = t & 1;
+                if (t >= 2 && !mbar_wait(smem_u32(acc_empty + b), (uint32_t)(((t - 2) >> 1) & 1), abort_flag)) break;
+                for (int j = 0; j < stages; ++j, ++it) {
+                    const int s = (int)(it % kS);
+                    if (!mbar_wait(smem_u32(full + s), (it / kS) & 1u, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const int steps = min(4, (p.k - j * kStageK + 63) / 64);   // products of 64 k; codes behind the last column are zero
+                    const uint32_t sc_t = tmem + (uint32_t)(kTmemScales + s * 16);
+                    for (int h = 0; 2 * h < steps; ++h) {
+                        tmem_copy_scales(sc_t + 4 * h, umma_desc_plain(smem_u32(smSc + s * 2048 + h * 512), 16));
+                        tmem_copy_scales(sc_t + 8 + 4 * h, umma_desc_plain(smem_u32(smSc + s * 2048 + 1024 + h * 512), 16));
+                    }
+                    const uint64_t ad = umma_desc_sw128(smem_u32(smA + s * C::kABytes)), bd = umma_desc_sw128(smem_u32(smB + s * C::kBBytes));
+                    for (int q = 0; q < steps; ++q)
+                        umma_mxf4(tmem + (uint32_t)(b * 128), ad + 2 * q, bd + 2 * q, umma_idesc_mxf4(kBM, kBN, (q & 1) * 2), sc_t + 4 * (q >> 1),
+                                  sc_t + 8 + 4 * (q >> 1), j > 0 || q > 0);
+                    umma_commit(smem_u32(empty + s));
+                }
+                if (ok) umma_commit(smem_u32(acc_full + b));
+            }
+        }
+        __syncwarp();
+    } else if (warp >= 4) {
+        constexpr int kCols = 128 / (int)sizeof(T);   // columns of a 128-byte piece of a row
+        constexpr int kPiece = kCols;
+        const int w = warp - 4;
+        unsigned char *stg = smOut + w * 4096;
+        int t = 0;
+        for (int64_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, ++t) {
+            const int b = t & 1;
+            if (!mbar_wait(smem_u32(acc_full + b), (uint32_t)((t >> 1) & 1), abort_flag)) break;
+            tc_fence_after();
+            const int64_t row0 = tile / p.n_tiles * kBM + w * 32;
+            const int n0 = (int)(tile % p.n_tiles) * kBN;
+#pragma unroll 1
+            for (int c0 = 0; c0 < kBN; c0 += kPiece) {
+                const int col = n0 + c0;
+#pragma unroll
+                for (int h = 0; h < kPiece; h += 32) {
+                    uint32_t r[32];
+                    tmem_ld32(tmem + ((uint32_t)(w * 32) << 16) + (uint32_t)(b * 128 + c0 + h), r);
+                    tmem_ld_wait();
+                    if (c0 + h + 32 == kBN) {   // all of it is in registers: the accumulator is free
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(acc_empty + b));
+                    }
+                    float v[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        v[i] = __uint_as_float(r[i]);
+                        if (p.bias) v[i] += col + h + i < p.n ? __ldg(p.bias + col + h + i) : 0.f;
+                        if (p.relu) v[i] = v[i] < 0.f ? 0.f : v[i];   // NaN stays
+                    }
+                    // 16-byte pieces of the row, in an order that keeps the lanes (one row each) on different banks
+#pragma unroll
+                    for (int q = 0; q < 32 * (int)sizeof(T) / 16; ++q) {
+                        uint4 o;
+                        if constexpr (sizeof(T) == 2) {
+                            uint32_t pk[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const __nv_bfloat162 hh = __floats2bfloat162_rn(v[8 * q + 2 * i], v[8 * q + 2 * i + 1]);
+                                pk[i] = *reinterpret_cast<const uint32_t *>(&hh);
+                            }
+                            o = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                        } else {
+                            o = make_uint4(__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
+                        }
+                        const int piece = h * (int)sizeof(T) / 16 + q;
+                        *reinterpret_cast<uint4 *>(stg + lane * 128 + ((piece ^ (lane & 7)) << 4)) = o;
+                    }
+                }
+                __syncwarp();
+                T *out = static_cast<T *>(p.out);
+                constexpr int kPer = 16 / (int)sizeof(T);          // elements of a 16-byte piece
+                constexpr int kLanes = kPiece * (int)sizeof(T) / 16;   // lanes to a row
+                const int lr = lane / kLanes, lp = lane % kLanes;
+#pragma unroll
+                for (int i = 0; i < kLanes; ++i) {
+                    const int r = i * (32 / kLanes) + lr;
+                    const int64_t row = row0 + r;
+                    const uint4 o = *reinterpret_cast<const uint4 *>(stg + r * 128 + ((lp ^ (r & 7)) << 4));
+                    const int c = col + lp * kPer;
+                    if (row < p.m && c < p.n) {
+                        T *dst = out + row * p.out_stride + c;
+                        if (p.wide && c + kPer <= p.n) *reinterpret_cast<uint4 *>(dst) = o;
+                        else {
+                            const T *e = reinterpret_cast<const T *>(&o);
+                            for (int x = 0; x < kPer && c + x < p.n; ++x) dst[x] = e[x];
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+
+    if (*abort_flag) {
+        if (tid == 0 && p.status) atomicOr(p.status, AIF_STATUS_TIMEOUT);
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000ll) __nanosleep(1000);   // copies in flight land before the memory is given up
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// Codes as a matrix of bytes [rows x cols / 2], boxes of 128 bytes x box_rows, 128-byte swizzle; columns and rows behind the end read as zero.
+cudaError_t encode_codes(CUtensorMap *m, const uint8_t *codes, int64_t rows, int cols, int box_rows)
+{
+    EncodeFn enc = encode_fn();
+    if (!enc) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {(cuuint64_t)(cols / 2), (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)(cols / 2)};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t *>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <typename T>
+cudaError_t run_gemm(GemmParams p, const uint8_t *a_codes, const uint8_t *w_codes, cudaStream_t st)
+{
+    using C = GemmCfg;
+    CUtensorMap ta, tw;
+    cudaError_t e = encode_codes(&ta, a_codes, p.m, p.k, kBM);
+    if (e == cudaSuccess) e = encode_codes(&tw, w_codes, p.n, p.k, kBN);
+    // (an attribute of the device's copy of the kernel: set for whichever device is current)
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_mx4_gemm<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+    if (e != cudaSuccess) return e;
+    p.n_tiles = (p.n + kBN - 1) / kBN;
+    p.tiles = (p.m + kBM - 1) / kBM * p.n_tiles;
+    const unsigned grid = (unsigned)(p.tiles < 148 ? p.tiles : 148);
+    e = launch_pdl(k_mx4_gemm<T>, dim3(grid), dim3(C::kThreads), C::kSmem, st, ta, tw, p);
+    count_launch();
+    return e;
+}
+
+}  // namespace
+}  // namespace aif
+
+using namespace aif;
+
+extern "C" {
+
+int64_t aif_mx4_workspace_bytes(int64_t m, int32_t k)
+{
+    const int64_t sc = aif_mx4_scale_bytes(m, k);
+    return sc < 0 ? sc : (m * (k / 2) + 255) / 256 * 256 + sc;
+}
+
+int aif_mx4_linear(const aif_mx4_product *q, aif_stream stream)
+{
+    StageRange range("aif_mx4_linear");
+    if (!q || q->struct_size != sizeof(aif_mx4_product)) return AIF_ERR_ARG;
+    if (q->dtype != AIF_F32 && q->dtype != AIF_BF16) return AIF_ERR_ARG;
+    if (q->m < 0 || q->m > INT_MAX - kBM || q->n < 1 || q->k < kMxBlock || q->k % kMxBlock != 0 || q->out_stride < q->n) return AIF_ERR_SHAPE;
+    if (q->n > INT_MAX - 128 || (q->m + 127) / 128 * mx_scale_tiles(q->k) > INT_MAX) return AIF_ERR_SHAPE;
+    if (q->m == 0) return AIF_OK;
+    auto aligned = [](const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+    const int el = q->dtype == AIF_BF16 ? 2 : 4;
+    if (!aligned(q->w_codes) || !aligned(q->w_scales) || !q->out || reinterpret_cast<uintptr_t>(q->out) % el != 0) return AIF_ERR_ARG;
+    if (q->bias && reinterpret_cast<uintptr_t>(q->bias) % 4 != 0) return AIF_ERR_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const uint8_t *codes = q->x_codes, *scales = q->x_scales;
+    cudaError_t e = cudaSuccess;
+    if (q->x) {
+        if (q->x_stride < q->k) return AIF_ERR_SHAPE;
+        if (reinterpret_cast<uintptr_t>(q->x) % el != 0 || !aligned(q->workspace) || q->workspace_bytes < aif_mx4_workspace_bytes(q->m, q->k)) return AIF_ERR_ARG;
+        uint8_t *ws = static_cast<uint8_t *>(q->workspace);
+        codes = ws, scales = ws + (q->m * (q->k / 2) + 255) / 256 * 256;
+        e = launch_mx4_quantize(q->x, q->dtype, q->m, q->k, q->x_stride, ws, const_cast<uint8_t *>(scales), st);
+    } else if (!aligned(codes) || !aligned(scales)) {
+        return AIF_ERR_ARG;
+    }
+    GemmParams p{};
+    p.m = q->m, p.n = q->n, p.k = q->k, p.a_scales = scales, p.w_scales = q->w_scales, p.bias = q->bias, p.relu = q->relu;
+    p.out = q->out, p.out_stride = q->out_stride, p.status = q->status;
+    p.wide = (reinterpret_cast<uintptr_t>(q->out) & 15) == 0 && (q->out_stride * el) % 16 == 0;
+    if (e == cudaSuccess) e = q->dtype == AIF_BF16 ? run_gemm<__nv_bfloat16>(p, codes, q->w_codes, st) : run_gemm<float>(p, codes, q->w_codes, st);
+    if (e == cudaSuccess) return AIF_OK;
+    char text[256];
+    snprintf(text, sizeof(text), "aif_mx4_linear: %s", cudaGetErrorString(e));
+    cudaGetLastError();
+    set_last_error(text);
+    return AIF_ERR_CUDA;
+}
+
+}  // extern "C"
