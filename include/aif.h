@@ -473,7 +473,7 @@ typedef struct {
     const void *q;             /* [rows x n_heads x d], q_stride elements from row to row; 16-byte aligned rows */
     void *out;                 /* likewise; may not overlap q */
     int64_t q_stride, out_stride;
-    float scale;               /* 0: 1 / sqrt(d) */
+    float scale;               /* > 0, or 0: 1 / sqrt(d) */
     int32_t window, sinks;     /* window 0: all rows are visible, sinks is not used */
     int32_t pad_;
     void *workspace;           /* aif_cache4_attention_workspace bytes, 16-byte aligned; not shared with a call that may run at the same time */

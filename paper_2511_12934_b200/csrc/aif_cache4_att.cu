@@ -1,11 +1,12 @@
 // Attention of query rows over sequences in the 4-bit cache: the CUDA-core kernel (fp32 models, and few rows per sequence, where the
 // work is to read the cache once), the kernel that joins pieces, and the entry points.
 //
-// k_att4_rows: R query rows of a sequence against all its visible keys.  A key row is spread over P lanes (32 of its elements, one block, to a lane for one
-// query row; 16 elements where R rows share the decoding), 32 / P keys to a warp step, each key group of lanes with a running maximum, weight and sum of its
-// own, so a step needs no exchange but the score's sum over P lanes.  Codes are decoded once for score and sum where values are the keys;
-// sums are fp32 throughout (f32x2 fused multiply-adds).  Codes and scales of a warp's next steps are in flight in registers while one is at work.
-// Bound: HBM (17/32 byte per element) or issue slots (2.5 instructions per element and row).
+// k_att4_rows: R query rows of a sequence against all its visible keys.  A warp takes stages of a few groups of 16 rows (a group lies in one page: its
+// codes and scales are two contiguous pieces), copied asynchronously into a ring of its own in shared memory, three stages ahead of
+// the one at work.  A key row is spread over P lanes (32 of its elements, one block, to a lane for one query row; 16 elements where R rows share the decoding), 32 / P
+// keys to a step, each key group of lanes with a running maximum, weight and sum of its own, so a step needs no exchange but the score's sum over P lanes.
+// Codes are decoded once for score and sum where values are the keys; sums are fp32 throughout (f32x2 fused multiply-adds on register pairs).
+// Bound: HBM (17/32 byte per element) or issue slots (about three instructions per element of one row).
 #include <algorithm>
 #include <cfloat>
 #include <cstdio>
@@ -16,25 +17,39 @@
 namespace aif {
 namespace {
 
-constexpr int kRowThreads = 256;
+constexpr int kRowThreads = 128;
 constexpr int kRowWarps = kRowThreads / 32;
-constexpr int kSteps = 4;          // steps whose codes a warp loads at a time
-constexpr int kRowBlock = 256;     // visible keys of a unit
+constexpr int kRing = 4;           // stages of a warp's ring
+constexpr int kRowGroups = 16;     // groups of 16 rows of a unit
 
-template <typename T>
-__device__ __forceinline__ float to_f32(T x) { return (float)x; }
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+template <int R, int P>
+struct RowsCfg {
+    static constexpr int E = R == 1 ? 32 : 16;                     // elements of a lane
+    static constexpr int KS = 32 / P;                              // keys of a step
+    static constexpr int kKeys = 4 * KS > 16 ? 4 * KS : 16;        // keys of a stage
+    static constexpr int kGroups = kKeys / 16;
+};
 
 template <typename T, int R, int P, bool SHARED>
-__global__ void __launch_bounds__(kRowThreads, R == 1 ? 2 : 1) k_att4_rows(const AttCall a)
+__global__ void __launch_bounds__(kRowThreads, 3) k_att4_rows(const AttCall a)
 {
-    constexpr int E = R == 1 ? 32 : 16;   // elements of a lane
-    constexpr int KS = 32 / P;            // keys of a step
-    constexpr int W = E / 8;              // code words of a lane
+    using C = RowsCfg<R, P>;
+    constexpr int E = C::E, KS = C::KS, W = E / 8, kKinds = SHARED ? 1 : 2;   // W: code words of a lane
     const Cache4 &c = a.c;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, d = c.d, nb = d >> 5;
     const int part = lane % P, sub = lane / P;
-    const bool act = part * E < c.d;
-    extern __shared__ float smem[];   // [warps][R][d + 2]
+    const bool act = part * E < d;
+    extern __shared__ __align__(16) unsigned char smem[];   // rings [warps][kRing][kKinds][codes, scales]; then sums [warps][R][d + 2]
+    const int stage_bytes = C::kKeys * (d / 2 + nb);
+    unsigned char *ring = smem + warp * (kRing * kKinds) * stage_bytes;
+    float *sums = reinterpret_cast<float *>(smem + kRowWarps * (kRing * kKinds) * stage_bytes);
     __shared__ PlanShared<kRowThreads> plan;
 
     grid_dep_wait();
@@ -47,116 +62,112 @@ __global__ void __launch_bounds__(kRowThreads, R == 1 ? 2 : 1) k_att4_rows(const
     const int64_t u1 = cut(total, ctas, cta + 1);
     int64_t u = cut(total, ctas, cta);
     Cursor cur = plan_find(a, plan, u);
-    const int d2 = c.d + 2;
+    const int d2 = d + 2;
     bool bad_page = false;
     while (u < u1) {
         const Entry &e = cur.e;
         const int row_tiles = cur.tiles / c.heads, head = cur.tile / row_tiles, r0 = (cur.tile - head * row_tiles) * R, rows = min(R, e.rows - r0);
         const int64_t tile_u0 = u - cur.block;
         const int take = (int)min(u1 - u, (int64_t)(cur.blocks - cur.block));
-        const int keys = e.keys(), k0 = cur.block * kRowBlock, k1 = min(keys, (cur.block + take) * kRowBlock);
+        const int groups = e.groups(), g0 = cur.block * kRowGroups, g1 = min(groups, (cur.block + take) * kRowGroups);
+        const int sink_groups = e.sink_groups(), rest_group = (e.rest >> 4) - sink_groups;
+        const int32_t *table = c.table + (size_t)max(e.seq, 0) * c.max_pages;
 
-        float2 q[R][E / 2], o[R][E / 2];
+        // the stage that begins with group `grp` into slot `slot` of the ring
+        auto bring = [&](int grp, int slot) {
+#pragma unroll
+            for (int x = 0; x < C::kGroups; ++x) {
+                const int gi = grp + x;
+                if (gi >= g1) break;
+                const int row = (gi < sink_groups ? gi : gi + rest_group) << 4, page = __ldg(table + (row >> c.page_shift));
+                const bool ok = c.holds(page);
+                bad_page |= !ok;
+                const size_t at = c.row(ok ? page : 0, head, row & (c.page_rows() - 1));
+#pragma unroll
+                for (int k = 0; k < kKinds; ++k) {
+                    unsigned char *codes = ring + (slot * kKinds + k) * stage_bytes + x * 16 * (d / 2), *scales = ring + (slot * kKinds + k) * stage_bytes + C::kKeys * (d / 2) + x * 16 * nb;
+                    const uint8_t *from = c.codes[k] + at * (d / 2);
+                    for (int y = lane; y < 16 * nb; y += 32) cp_async16(smem_u32(codes + y * 16), from + y * 16, 16u);
+                    if (ok) {
+                        if (lane < nb) cp_async16(smem_u32(scales + lane * 16), c.scales[k] + at * nb + lane * 16, 16u);
+                    } else {   // no such page: no number
+                        for (int y = lane; y < 16 * nb; y += 32) scales[y] = (unsigned char)kMxNan;
+                    }
+                }
+            }
+            cp_async_commit();
+        };
+        const int first = g0 + warp * C::kGroups;
+        constexpr int kStride = kRowWarps * C::kGroups;
+#pragma unroll
+        for (int i = 0; i < kRing - 1; ++i) {
+            if (first + i * kStride < g1) bring(first + i * kStride, i);
+            else cp_async_commit();
+        }
+
+        uint64_t q[R][E / 2], o[R][E / 2];
         float m[R], l[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             m[r] = -FLT_MAX, l[r] = 0.f;
             const int rr = min(r, rows - 1) + r0, query = rr / a.group;
-            const T *src = static_cast<const T *>(a.q) + (e.row0 + query) * a.q_stride + (head * a.group + rr - query * a.group) * c.d + part * E;
+            const T *src = static_cast<const T *>(a.q) + (e.row0 + query) * a.q_stride + (head * a.group + rr - query * a.group) * d + part * E;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 float v[8] = {};
                 if (act) load8<T, true>(src + w * 8, v);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    q[r][w * 4 + i] = make_float2(v[2 * i] * a.scale_log2, v[2 * i + 1] * a.scale_log2);
-                    o[r][w * 4 + i] = make_float2(0.f, 0.f);
-                }
+                for (int i = 0; i < 4; ++i) q[r][w * 4 + i] = pack_f32x2(v[2 * i] * a.scale_log2, v[2 * i + 1] * a.scale_log2), o[r][w * 4 + i] = 0ull;
             }
         }
-        const int32_t *table = c.table + (size_t)max(e.seq, 0) * c.max_pages;
-        constexpr int kChunk = kSteps * KS;
-
-        uint32_t kc[kSteps][W], vc[SHARED ? 1 : kSteps][W];
-        float ks[kSteps], vs[SHARED ? 1 : kSteps];
-        auto fetch = [&](int v0) {   // codes and scales of the chunk at visible key v0 (zero weight and zero codes behind the end)
+        int slot = 0;
+        for (int grp = first; grp < g1; grp += kStride) {
+            // (the slot that is filled now was read a whole stage ago)
+            const int ahead = grp + (kRing - 1) * kStride;
+            if (ahead < g1) bring(ahead, (slot + kRing - 1) % kRing);
+            else cp_async_commit();
+            cp_async_wait<kRing - 1>();
+            __syncwarp();
+            const unsigned char *codes = ring + slot * kKinds * stage_bytes, *scales = codes + C::kKeys * (d / 2);
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                const int v = v0 + s * KS + sub;
-#pragma unroll
-                for (int w = 0; w < W; ++w) kc[s][w] = 0u;
-                ks[s] = 0.f;
-                if (!SHARED) {
-#pragma unroll
-                    for (int w = 0; w < W; ++w) vc[s][w] = 0u;
-                    vs[s] = 0.f;
-                }
-                if (v >= k1 || !act) continue;
-                const int key = e.key(v), page = __ldg(table + (key >> c.page_shift));
-                if (!c.holds(page)) {
-                    bad_page = true, ks[s] = NAN;
-                    continue;
-                }
-                const size_t row = c.row(page, head, key & (c.page_rows() - 1));
-                auto load = [&](int which, uint32_t (&to)[W], float &scale) {
-                    const uint8_t *p = c.codes[which] + row * (c.d / 2) + part * (E / 2);
-                    if constexpr (W == 4) {
-                        const uint4 x = __ldg(reinterpret_cast<const uint4 *>(p));
-                        to[0] = x.x, to[1] = x.y, to[2] = x.z, to[3] = x.w;
-                    } else {
-                        const uint2 x = __ldg(reinterpret_cast<const uint2 *>(p));
-                        to[0] = x.x, to[1] = x.y;
-                    }
-                    scale = mx_scale(__ldg(c.scales[which] + row * (c.d / 32) + part * E / 32));
-                };
-                load(0, kc[s], ks[s]);
-                if constexpr (!SHARED) load(1, vc[s], vs[s]);
-            }
-        };
-        int v0 = k0 + warp * kChunk;
-        if (v0 < k1) fetch(v0);
-        for (; v0 < k1; v0 += kRowWarps * kChunk) {
-            uint32_t kn[kSteps][W], vn[SHARED ? 1 : kSteps][W];
-            float kns[kSteps], vns[SHARED ? 1 : kSteps];
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
-                kns[s] = ks[s];
-#pragma unroll
-                for (int w = 0; w < W; ++w) kn[s][w] = kc[s][w];
-                if constexpr (!SHARED) {
-                    vns[s] = vs[s];
-#pragma unroll
-                    for (int w = 0; w < W; ++w) vn[s][w] = vc[s][w];
-                }
-            }
-            if (v0 + kRowWarps * kChunk < k1) fetch(v0 + kRowWarps * kChunk);
-#pragma unroll
-            for (int s = 0; s < kSteps; ++s) {
+            for (int s = 0; s < C::kKeys / KS; ++s) {
+                const int k = s * KS + sub, gi = grp + (k >> 4);
+                const int row = ((gi < sink_groups ? gi : gi + rest_group) << 4) + (k & 15);
+                const bool there = gi < g1 && (gi < sink_groups ? row < e.first : row >= e.rest && row < e.length);
                 uint64_t val[E / 2];
-                auto decode = [&](const uint32_t (&codes)[W]) {
+                auto decode = [&](const unsigned char *from) {
+                    uint32_t w[W];
+                    if constexpr (W == 4) {
+                        const uint4 x = *reinterpret_cast<const uint4 *>(from);
+                        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(from);
+                        w[0] = x.x, w[1] = x.y;
+                    }
 #pragma unroll
-                    for (int w = 0; w < W; ++w) {
+                    for (int i = 0; i < W; ++i) {
                         uint32_t h[4];
-                        mx_decode8_f16(codes[w], h);
+                        mx_decode8_f16(w[i], h);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float2 f = half2_to_float2(h[i]);
-                            val[w * 4 + i] = pack_f32x2(f.x, f.y);
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 f = half2_to_float2(h[j]);
+                            val[i * 4 + j] = pack_f32x2(f.x, f.y);
                         }
                     }
                 };
-                decode(kn[s]);
-                const bool there = v0 + s * KS + sub < k1;
+                const int cell = k * (d / 2) + (act ? part * (E / 2) : 0), cell_scale = k * nb + (act ? part * E / 32 : 0);
+                decode(codes + cell);
+                float scale = there && act ? mx_scale(scales[cell_scale]) : 0.f;   // (what is not there has finite codes and no scale)
                 float pr[R];
                 bool raise = false;
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    uint64_t acc = 0ull;
+                    uint64_t acc[2] = {0ull, 0ull};
 #pragma unroll
-                    for (int i = 0; i < E / 2; ++i) acc = fma_f32x2(val[i], pack_f32x2(q[r][i].x, q[r][i].y), acc);
+                    for (int i = 0; i < E / 2; ++i) acc[i & 1] = fma_f32x2(val[i], q[r][i], acc[i & 1]);
                     float x, y;
-                    unpack_f32x2(acc, x, y);
-                    float sc = (x + y) * kns[s];   // (a block of zero codes behind d: 0 x 0)
+                    unpack_f32x2(add_f32x2(acc[0], acc[1]), x, y);
+                    float sc = (x + y) * scale;
 #pragma unroll
                     for (int b = 1; b < P; b <<= 1) sc += __shfl_xor_sync(0xffffffffu, sc, b);
                     pr[r] = there ? sc : -INFINITY;
@@ -168,26 +179,28 @@ __global__ void __launch_bounds__(kRowThreads, R == 1 ? 2 : 1) k_att4_rows(const
                     for (int r = 0; r < R; ++r) {
                         const float mn = pr[r] > m[r] + 8.f ? pr[r] : m[r], f = fast_exp2(m[r] - mn);
                         m[r] = mn, l[r] *= f;
+                        const uint64_t ff = pack_f32x2(f, f);
 #pragma unroll
-                        for (int i = 0; i < E / 2; ++i) o[r][i].x *= f, o[r][i].y *= f;
+                        for (int i = 0; i < E / 2; ++i) o[r][i] = mul_f32x2(o[r][i], ff);
                     }
                 }
-                if constexpr (!SHARED) decode(vn[s]);
-                const float scale = SHARED ? kns[s] : vns[SHARED ? 0 : s];
+                if constexpr (!SHARED) {
+                    decode(codes + stage_bytes + cell);
+                    scale = there && act ? mx_scale(scales[stage_bytes + cell_scale]) : 0.f;
+                }
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const float pe = fast_exp2(pr[r] - m[r]);
                     l[r] += pe;
-                    const float pv = there ? pe * scale : 0.f;
-                    const uint64_t pp = pack_f32x2(pv, pv);
+                    const uint64_t pp = pack_f32x2(pe * scale, pe * scale);
 #pragma unroll
-                    for (int i = 0; i < E / 2; ++i) {
-                        const uint64_t t = fma_f32x2(val[i], pp, pack_f32x2(o[r][i].x, o[r][i].y));
-                        unpack_f32x2(t, o[r][i].x, o[r][i].y);
-                    }
+                    for (int i = 0; i < E / 2; ++i) o[r][i] = fma_f32x2(val[i], pp, o[r][i]);
                 }
             }
+            __syncwarp();
+            slot = (slot + 1) % kRing;
         }
+        cp_async_wait_all();
         // key groups of the warp, then the warps
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -198,39 +211,40 @@ __global__ void __launch_bounds__(kRowThreads, R == 1 ? 2 : 1) k_att4_rows(const
             float lt = l[r] * f;
 #pragma unroll
             for (int b = P; b < 32; b <<= 1) lt += __shfl_xor_sync(0xffffffffu, lt, b);
-            float *to = smem + (warp * R + r) * d2;
+            float *to = sums + (warp * R + r) * d2;
 #pragma unroll
             for (int i = 0; i < E / 2; ++i) {
-                float x = o[r][i].x * f, y = o[r][i].y * f;
+                float x, y;
+                unpack_f32x2(o[r][i], x, y);
+                x *= f, y *= f;
 #pragma unroll
                 for (int b = P; b < 32; b <<= 1) x += __shfl_xor_sync(0xffffffffu, x, b), y += __shfl_xor_sync(0xffffffffu, y, b);
                 if (sub == 0 && act) to[part * E + 2 * i] = x, to[part * E + 2 * i + 1] = y;
             }
-            if (lane == 0) to[c.d] = mt, to[c.d + 1] = lt;
+            if (lane == 0) to[d] = mt, to[d + 1] = lt;
         }
         __syncthreads();
         const bool begins = cur.block == 0, ends = cur.block + take == cur.blocks;
-        const int slot = 2 * cta + (begins ? 1 : 0);
-        float *rec = a.records + (size_t)slot * R * d2;
-        for (int x = tid; x < rows * c.d; x += kRowThreads) {
-            const int r = x / c.d, col = x - r * c.d;
+        float *rec = a.records + (size_t)(2 * cta + (begins ? 1 : 0)) * R * d2;
+        for (int x = tid; x < rows * d; x += kRowThreads) {
+            const int r = x / d, col = x - r * d;
             float mt = -FLT_MAX, sum = 0.f, weight = 0.f;
 #pragma unroll
-            for (int w = 0; w < kRowWarps; ++w) mt = fmaxf(mt, smem[(w * R + r) * d2 + c.d]);
+            for (int w = 0; w < kRowWarps; ++w) mt = fmaxf(mt, sums[(w * R + r) * d2 + d]);
 #pragma unroll
             for (int w = 0; w < kRowWarps; ++w) {
-                const float *from = smem + (w * R + r) * d2;
-                const float f = fast_exp2(from[c.d] - mt);
-                sum += from[col] * f, weight += from[c.d + 1] * f;
+                const float *from = sums + (w * R + r) * d2;
+                const float f = fast_exp2(from[d] - mt);
+                sum += from[col] * f, weight += from[d + 1] * f;
             }
             if (begins && ends) {
                 const int rr = r0 + r, query = rr / a.group;
-                T *dst = static_cast<T *>(a.out) + (e.row0 + query) * a.out_stride + (head * a.group + rr - query * a.group) * c.d + col;
+                T *dst = static_cast<T *>(a.out) + (e.row0 + query) * a.out_stride + (head * a.group + rr - query * a.group) * d + col;
                 // (no keys: a zero row; a bad sequence: no number)
-                *dst = (T)(e.length < 0 ? NAN : keys == 0 ? 0.f : sum / weight);
+                *dst = (T)(e.length < 0 ? NAN : groups == 0 ? 0.f : sum / weight);
             } else {
-                rec[r * c.d + col] = sum;
-                if (col == 0) rec[R * c.d + 2 * r] = mt, rec[R * c.d + 2 * r + 1] = weight;
+                rec[r * d + col] = sum;
+                if (col == 0) rec[R * d + 2 * r] = mt, rec[R * d + 2 * r + 1] = weight;
             }
         }
         if (ends && !begins && tid == 0) {
@@ -278,36 +292,42 @@ __global__ void __launch_bounds__(256) k_att4_join(const AttCall a, int permuted
 
 bool at16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+template <typename T, int R, int P, bool SHARED>
+cudaError_t run_rows_at(const AttCall &a, int grid, cudaStream_t st)
+{
+    const size_t smem = (size_t)kRowWarps * kRing * (SHARED ? 1 : 2) * RowsCfg<R, P>::kKeys * (a.c.d / 2 + a.c.d / 32) + (size_t)kRowWarps * R * (a.c.d + 2) * 4;
+    // (an attribute of the device's copy of the kernel: set for whichever device is current)
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(k_att4_rows<T, R, P, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    count_launch();
+    return launch_pdl(k_att4_rows<T, R, P, SHARED>, dim3(grid), dim3(kRowThreads), smem, st, a);
+}
 template <typename T, int R, bool SHARED>
 cudaError_t run_rows(const AttCall &a, int grid, cudaStream_t st)
 {
-    const size_t smem = (size_t)kRowWarps * R * (a.c.d + 2) * 4;   // 33 KB at most
-    const int lanes = (a.c.d + (R == 1 ? 31 : 15)) / (R == 1 ? 32 : 16);
-    auto go = [&](auto kernel) { return launch_pdl(kernel, dim3(grid), dim3(kRowThreads), smem, st, a); };
-    count_launch();
-    constexpr int kF = R == 1 ? 1 : 2;
-    if (lanes <= kF) return go(k_att4_rows<T, R, kF, SHARED>);
-    if (lanes <= 2 * kF) return go(k_att4_rows<T, R, 2 * kF, SHARED>);
-    if (lanes <= 4 * kF) return go(k_att4_rows<T, R, 4 * kF, SHARED>);
-    return go(k_att4_rows<T, R, 8 * kF, SHARED>);
+    constexpr int kF = R == 1 ? 1 : 2;   // lanes to a block of 32 elements
+    const int blocks = a.c.d / 32;
+    if (blocks <= 1) return run_rows_at<T, R, kF, SHARED>(a, grid, st);
+    if (blocks <= 2) return run_rows_at<T, R, 2 * kF, SHARED>(a, grid, st);
+    if (blocks <= 4) return run_rows_at<T, R, 4 * kF, SHARED>(a, grid, st);
+    return run_rows_at<T, R, 8 * kF, SHARED>(a, grid, st);
 }
 
 // How a call is run: which kernel, and how far it may be cut.
 struct AttForm {
-    bool tensor;      // the tensor-core kernel: tiles of 128 rows
+    enum { kRows, kFew, kPair, kTensor } kernel;
     int tile_rows, block_keys, grid, min_units;
 };
 AttForm form_of(const aif_cache4 *c, const aif_cache4_query *q)
 {
-    AttForm f{};
-    const int64_t group = q->n_heads / c->heads, per_seq = (q->rows + q->n - 1) / q->n * group;
-    f.tensor = q->dtype == AIF_BF16 && att4_tc_block_keys(c->d) > 0 && per_seq > 8;
-    if (f.tensor) {
-        f.tile_rows = 128, f.block_keys = att4_tc_block_keys(c->d), f.grid = 148, f.min_units = 4;
-    } else {
-        f.tile_rows = per_seq <= 1 ? 1 : 4, f.block_keys = kRowBlock, f.grid = per_seq <= 1 ? 296 : 148, f.min_units = 1;
-    }
-    return f;
+    const int64_t group = q->n_heads / c->heads, per_seq = (q->rows + q->n - 1) / q->n * group;   // query rows of a sequence and a head of the cache, on average
+    const bool bf = q->dtype == AIF_BF16;
+    if (bf && per_seq > 32 && (c->d == 64 || c->d == 128)) return {AttForm::kPair, 256, 64, 148, 4};
+    if (bf && per_seq > 32 && c->d == 256) return {AttForm::kTensor, 128, 64, 148, 4};
+    if (bf && per_seq > 2 && (c->d == 32 || c->d == 64 || c->d == 128 || c->d == 256)) return {AttForm::kFew, 8, -32, c->d == 256 ? 148 : 296, 1};
+    return {AttForm::kRows, per_seq <= 2 ? 1 : 4, -kRowGroups, 444, 1};
 }
 int64_t workspace_of(const AttForm &f, const aif_cache4 *c)
 {
@@ -327,7 +347,7 @@ int check_query(const aif_cache4 *c, const aif_cache4_query *q)
     const int64_t width = (int64_t)q->n_heads * c->d, el = q->dtype == AIF_BF16 ? 2 : 4;
     if (q->q_stride < width || q->out_stride < width || q->q_stride * el % 16 != 0 || q->out_stride * el % 16 != 0) return AIF_ERR_SHAPE;
     if (q->window < 0 || q->sinks < 0) return AIF_ERR_SHAPE;
-    if (!(q->scale == q->scale) || q->scale - q->scale != 0.f) return AIF_ERR_ARG;   // NaN, infinite
+    if (!(q->scale >= 0.f) || q->scale - q->scale != 0.f) return AIF_ERR_ARG;   // (NaN, infinite)
     return AIF_OK;
 }
 
@@ -364,7 +384,9 @@ int aif_cache4_attention(const aif_cache4 *c, const aif_cache4_query *q, aif_str
     a.records = reinterpret_cast<float *>(a.headers + f.grid);
     const bool bf = q->dtype == AIF_BF16, shared = c->shared != 0;
     cudaError_t e;
-    if (f.tensor) e = launch_att4_tc(a, f.grid, st);
+    if (f.kernel == AttForm::kPair) e = launch_att4_pair(a, f.grid, st);
+    else if (f.kernel == AttForm::kTensor) e = launch_att4_tc(a, f.grid, st);
+    else if (f.kernel == AttForm::kFew) e = launch_att4_few(a, f.grid, st);
     else if (f.tile_rows == 1)
         e = bf ? (shared ? run_rows<__nv_bfloat16, 1, true>(a, f.grid, st) : run_rows<__nv_bfloat16, 1, false>(a, f.grid, st))
                : (shared ? run_rows<float, 1, true>(a, f.grid, st) : run_rows<float, 1, false>(a, f.grid, st));
@@ -372,8 +394,9 @@ int aif_cache4_attention(const aif_cache4 *c, const aif_cache4_query *q, aif_str
         e = bf ? (shared ? run_rows<__nv_bfloat16, 4, true>(a, f.grid, st) : run_rows<__nv_bfloat16, 4, false>(a, f.grid, st))
                : (shared ? run_rows<float, 4, true>(a, f.grid, st) : run_rows<float, 4, false>(a, f.grid, st));
     if (e == cudaSuccess) {
-        const dim3 grid(f.grid, f.tensor ? 16 : 1);
-        e = bf ? launch_pdl(k_att4_join<__nv_bfloat16>, grid, dim3(256), 0, st, a, f.tensor ? 1 : 0) : launch_pdl(k_att4_join<float>, grid, dim3(256), 0, st, a, 0);
+        const bool tensor = f.kernel == AttForm::kPair || f.kernel == AttForm::kTensor;
+        const dim3 grid(f.grid, tensor ? f.tile_rows / 16 : 1);
+        e = bf ? launch_pdl(k_att4_join<__nv_bfloat16>, grid, dim3(256), 0, st, a, tensor ? 1 : 0) : launch_pdl(k_att4_join<float>, grid, dim3(256), 0, st, a, 0);
         count_launch();
     }
     return cache4_failed(e, "aif_cache4_attention");

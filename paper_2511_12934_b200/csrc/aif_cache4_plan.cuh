@@ -38,6 +38,10 @@ struct Entry {
     __device__ int keys() const { return length < 0 ? 0 : first + (length - rest); }
     // row of the visible key v
     __device__ int key(int v) const { return v < first ? v : rest + (v - first); }
+    // The same in groups of 16 rows that begin on multiples of 16 (and so lie in one page): groups of the call, and the first row of one.  Rows of a group
+    // that are not visible: at or behind `first` in the groups of the first rows, before `rest` in the others.
+    __device__ int sink_groups() const { return (first + 15) >> 4; }
+    __device__ int groups() const { return length < 0 ? 0 : sink_groups() + ((length + 15) >> 4) - (rest >> 4); }
 };
 
 // A tile as the CTA that finishes it hands it to the kernel that joins its pieces.
@@ -48,9 +52,9 @@ struct PieceHeader {
     int32_t pad_[2];
 };
 
-// Attention on the tensor cores (aif_cache4_tc.cu): bf16, d = 64, 128, 256.
-int att4_tc_block_keys(int d);   // keys of a unit; 0: d is not supported
-cudaError_t launch_att4_tc(const AttCall &a, int grid, cudaStream_t st);
+cudaError_t launch_att4_pair(const AttCall &a, int grid, cudaStream_t st);   // aif_cache4_pair.cu: bf16, d = 64, 128; tiles of 256 rows, blocks of 64 keys
+cudaError_t launch_att4_tc(const AttCall &a, int grid, cudaStream_t st);     // aif_cache4_tc.cu: bf16, d = 256; 128 rows, 64 keys
+cudaError_t launch_att4_few(const AttCall &a, int grid, cudaStream_t st);    // aif_cache4_few.cu: bf16, d = 32, 64, 128, 256; 8 rows, 512 keys
 
 namespace {
 
@@ -65,11 +69,15 @@ __device__ __forceinline__ Entry entry_at(const AttCall &a, int i)
         const int L = a.c.lengths[e.seq];
         if (L >= 0 && L <= a.c.longest()) e.length = L;
     }
-    e.first = max(e.length, 0), e.rest = e.first;
+    e.first = 0, e.rest = 0;
     if (a.window > 0 && e.length > a.window) e.rest = e.length - a.window, e.first = min(a.sinks, e.rest);
     return e;
 }
-__device__ __forceinline__ int blocks_at(const AttCall &a, const Entry &e) { return max(1, (int)(((int64_t)e.keys() + a.block_keys - 1) / a.block_keys)); }
+// (block_keys < 0: blocks of that many groups of 16 rows)
+__device__ __forceinline__ int blocks_at(const AttCall &a, const Entry &e)
+{
+    return max(1, a.block_keys > 0 ? (int)(((int64_t)e.keys() + a.block_keys - 1) / a.block_keys) : (e.groups() - a.block_keys - 1) / -a.block_keys);
+}
 __device__ __forceinline__ int tiles_at(const AttCall &a, const Entry &e) { return (e.rows + a.tile_rows - 1) / a.tile_rows; }
 __device__ __forceinline__ int64_t units_at(const AttCall &a, const Entry &e) { return (int64_t)tiles_at(a, e) * a.c.heads * blocks_at(a, e); }
 

@@ -1,4 +1,4 @@
-// Attention of many query rows over sequences in the 4-bit cache on the tensor cores (sm_100a), bf16, d = 64, 128, 256:
+// Attention of many query rows over sequences in the 4-bit cache on the tensor cores (sm_100a), bf16, d = 256:
 //   out_i = softmax_j(scale q_i k_j) v   for tiles of 128 query rows (queries x heads of a group) of one sequence.
 //
 // The 4-bit codes are unpacked to bf16 on their way into shared memory (exact: two significant bits and a power of two), once per tile and
@@ -8,7 +8,7 @@
 //          exponentials in fp32, probabilities back to tensor memory as bf16 pairs; at the end of a tile they normalise and store its rows
 //   8, 9   one lane issues scores = Q K^T up to two blocks ahead, one lane O += P V with V read MN-major from the tile K was read from
 //   10, 11 bring the query rows of the next tile
-//   12-15  unpack keys and values: a thread takes a key row (half of one at d = 256); its codes for the next block are in flight in registers
+//   12-15  unpack keys and values: a thread takes half of a key row; its codes for the next block are in flight in registers
 //          meanwhile, and the page numbers for the one after that
 // Eight codes of a word come apart as the pairs (0,4) (1,5) (2,6) (3,7) with two shifts, two masks and a multiplication each; queries are put
 // into the same order as they are brought, and sums are taken out of it as they are stored.
@@ -21,12 +21,14 @@
 namespace aif {
 namespace {
 
-template <int D, bool SHARED>
+constexpr int D = 256;   // (sums of two halves of 256 rows, as for smaller d, would fill all of tensor memory)
+
+template <bool SHARED>
 struct Att4Cfg {
-    static constexpr int kBN = D == 256 ? 64 : 128;       // keys of a block: two score buffers, two of probabilities and O fill 512 columns
+    static constexpr int kBN = 64;                        // keys of a block: two score buffers, two of probabilities and O fill 512 columns
     static constexpr int kChunks = D / 64;                // 64-column (128-byte) chunks of a row
     static constexpr int kQBytes = kChunks * 128 * 128;
-    static constexpr int kQBufs = D == 256 ? 1 : 2;
+    static constexpr int kQBufs = 1;
     static constexpr int kChunkBytes = kBN * 128;
     static constexpr int kTileBytes = kChunks * kChunkBytes;
     static constexpr int kKinds = SHARED ? 1 : 2;
@@ -40,42 +42,10 @@ struct Att4Cfg {
     static constexpr size_t kSmem = 1024 + kQBufs * kQBytes + kStages * kStageBytes + kOutBytes + kMisc;
 };
 
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
-{
-    uint32_t o;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
-    return o;
-}
-
-// Eight codes to four bf16 pairs.  A code's exponent and mantissa bits are put where bf16 has its lowest exponent bits and its highest mantissa bit:
-// the value times 2^-126, subnormal codes included, and one exact multiplication by 2^126 times the block's scale makes it the value.
-// Scales beyond 2 (byte > 128) would need a factor beyond the largest power of two: they take two steps.
-struct UnpackScale {
-    uint32_t first, second;   // bf16 pairs
-    bool two;
-    __device__ __forceinline__ explicit UnpackScale(uint32_t byte)
-    {
-        two = byte > 128u;
-        const uint32_t f = two ? 253u << 7 : (byte + 126u) << 7, s = byte == kMxNan ? 0x7fffu : byte << 7;
-        first = f | (f << 16), second = s | (s << 16);
-    }
-};
-__device__ __forceinline__ uint4 unpack8(uint32_t w, const UnpackScale &s)
-{
-    uint4 o;
-    o.x = ((w << 12) & 0x80008000u) | ((w << 6) & 0x01c001c0u);
-    o.y = ((w << 8) & 0x80008000u) | ((w << 2) & 0x01c001c0u);
-    o.z = ((w << 4) & 0x80008000u) | ((w >> 2) & 0x01c001c0u);
-    o.w = (w & 0x80008000u) | ((w >> 6) & 0x01c001c0u);
-    o.x = mul_bf16x2(o.x, s.first), o.y = mul_bf16x2(o.y, s.first), o.z = mul_bf16x2(o.z, s.first), o.w = mul_bf16x2(o.w, s.first);
-    if (s.two) o.x = mul_bf16x2(o.x, s.second), o.y = mul_bf16x2(o.y, s.second), o.z = mul_bf16x2(o.z, s.second), o.w = mul_bf16x2(o.w, s.second);
-    return o;
-}
-
-template <int D, bool SHARED>
+template <bool SHARED>
 __global__ void __launch_bounds__(512, 1) k_att4_tc(const AttCall a)
 {
-    using C = Att4Cfg<D, SHARED>;
+    using C = Att4Cfg<SHARED>;
     constexpr int BN = C::kBN, kS = C::kStages, kQB = C::kQBufs;
     extern __shared__ unsigned char smem_dyn[];
     unsigned char *base = reinterpret_cast<unsigned char *>(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
@@ -180,13 +150,6 @@ __global__ void __launch_bounds__(512, 1) k_att4_tc(const AttCall a)
                             if (i < vc) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(sc[i]));
                     }
                     mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * k2;
-                    // (a negative scale turns the order round)
-                    if (k2 < 0.f) {
-                        mt = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < CW; ++i)
-                            if (i < vc) mt = fmaxf(mt, __uint_as_float(sc[i]) * k2);
-                    }
                 }
                 // the two warps of a quarter agree on the block's maximum (two buffers: the partner may still read the block before)
                 float *mx = mx_s + (gb & 1u) * 256;
@@ -451,7 +414,7 @@ __global__ void __launch_bounds__(512, 1) k_att4_tc(const AttCall a)
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) next[k].w[b] = __ldg(p + b);
                 const uint8_t *ps = c.scales[k] + row * (D / 32) + b0;
-                next[k].sc[0] = kBlk == 2 ? __ldg(reinterpret_cast<const uint16_t *>(ps)) : __ldg(reinterpret_cast<const uint32_t *>(ps));
+                next[k].sc[0] = __ldg(reinterpret_cast<const uint32_t *>(ps));
             }
         };
         int page = -1, in_page = 0, head = 0;
@@ -502,29 +465,22 @@ __global__ void __launch_bounds__(512, 1) k_att4_tc(const AttCall a)
     if (warp == C::kQkWarp) tmem_dealloc(tmem, 512);
 }
 
-template <int D, bool SHARED>
+template <bool SHARED>
 cudaError_t run_tc(const AttCall &a, int grid, cudaStream_t st)
 {
-    using C = Att4Cfg<D, SHARED>;
+    using C = Att4Cfg<SHARED>;
     // (an attribute of the device's copy of the kernel: set for whichever device is current)
-    cudaError_t e = cudaFuncSetAttribute(k_att4_tc<D, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+    cudaError_t e = cudaFuncSetAttribute(k_att4_tc<SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
     if (e != cudaSuccess) return e;
     count_launch();
-    return launch_pdl(k_att4_tc<D, SHARED>, dim3(grid), dim3(C::kThreads), C::kSmem, st, a);
+    return launch_pdl(k_att4_tc<SHARED>, dim3(grid), dim3(C::kThreads), C::kSmem, st, a);
 }
 
 }  // namespace
 
-int att4_tc_block_keys(int d) { return d == 64 || d == 128 ? 128 : d == 256 ? 64 : 0; }
-
 cudaError_t launch_att4_tc(const AttCall &a, int grid, cudaStream_t st)
 {
-    const bool shared = a.c.codes[0] == a.c.codes[1];
-    switch (a.c.d) {
-        case 64: return shared ? run_tc<64, true>(a, grid, st) : run_tc<64, false>(a, grid, st);
-        case 128: return shared ? run_tc<128, true>(a, grid, st) : run_tc<128, false>(a, grid, st);
-        default: return shared ? run_tc<256, true>(a, grid, st) : run_tc<256, false>(a, grid, st);
-    }
+    return a.c.codes[0] == a.c.codes[1] ? run_tc<true>(a, grid, st) : run_tc<false>(a, grid, st);
 }
 
 }  // namespace aif

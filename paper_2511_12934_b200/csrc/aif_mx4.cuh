@@ -124,6 +124,38 @@ __device__ __forceinline__ void mx_values8(uint32_t codes, float scale, float (&
     }
 }
 
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t o;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
+    return o;
+}
+
+// Eight codes to four bf16 pairs.  A code's exponent and mantissa bits are put where bf16 has its lowest exponent bits and its highest mantissa bit:
+// the value times 2^-126, subnormal codes included, and one exact multiplication by 2^126 times the block's scale makes it the value.
+// Scales beyond 2 (byte > 128) would need a factor beyond the largest power of two: they take two steps.
+struct UnpackScale {
+    uint32_t first, second;   // bf16 pairs
+    bool two;
+    __device__ __forceinline__ explicit UnpackScale(uint32_t byte)
+    {
+        two = byte > 128u;
+        const uint32_t f = two ? 253u << 7 : (byte + 126u) << 7, s = byte == kMxNan ? 0x7fffu : byte << 7;
+        first = f | (f << 16), second = s | (s << 16);
+    }
+};
+__device__ __forceinline__ uint4 unpack8(uint32_t w, const UnpackScale &s)
+{
+    uint4 o;
+    o.x = ((w << 12) & 0x80008000u) | ((w << 6) & 0x01c001c0u);
+    o.y = ((w << 8) & 0x80008000u) | ((w << 2) & 0x01c001c0u);
+    o.z = ((w << 4) & 0x80008000u) | ((w >> 2) & 0x01c001c0u);
+    o.w = (w & 0x80008000u) | ((w >> 6) & 0x01c001c0u);
+    o.x = mul_bf16x2(o.x, s.first), o.y = mul_bf16x2(o.y, s.first), o.z = mul_bf16x2(o.z, s.first), o.w = mul_bf16x2(o.w, s.first);
+    if (s.two) o.x = mul_bf16x2(o.x, s.second), o.y = mul_bf16x2(o.y, s.second), o.z = mul_bf16x2(o.z, s.second), o.w = mul_bf16x2(o.w, s.second);
+    return o;
+}
+
 // Scale bytes of a matrix lie in tiles of 128 rows x 4 blocks, 512 bytes each, the tiles of a band of 128 rows one after the other:
 // byte (row, block) at (row / 128 * tiles + block / 4) * 512 + row % 32 * 16 + row % 128 / 32 * 4 + block % 4, which is the order in
 // which the block-scaled products read 32 rows x 16 bytes into tensor memory.

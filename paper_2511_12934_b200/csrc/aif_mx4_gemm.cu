@@ -4,8 +4,8 @@
 //
 // One CTA per SM walks over tiles of 128 rows x 128 columns, columns fastest, so that the rows of a tile come from HBM once and from
 // L2 for the other columns.  Warps: 0 streams stages of 256 k (128 bytes of codes per row by TMA, the scale tiles by bulk copies);
-// 1 copies a stage's scales to tensor memory and issues its four products of 64 k; 4-7 take a finished accumulator out of tensor memory while the
-// next tile is at work (two accumulators), stage it in shared memory and store whole 128-byte pieces of rows.
+// 1 copies a stage's scales to tensor memory and issues its four products of 64 k; 4-11 take a finished accumulator out of tensor memory while the
+// next tile is at work (two accumulators) and store it through shared memory with asynchronous tile stores.
 // The scale copies go to tensor-memory columns of their own per stage: a stage is only refilled once its products have completed.
 #include <climits>
 #include <cstdio>
@@ -52,10 +52,10 @@ constexpr int kBN = 128;
 struct GemmCfg {
     static constexpr int kABytes = kBM * 128, kBBytes = kBN * 128;
     static constexpr int kStageBytes = kABytes + kBBytes + 2048;   // + two scale tiles of each operand
-    static constexpr int kStages = 5;
-    static constexpr int kThreads = 256;
-    static constexpr int kOutBytes = 4 * 4096;                     // 32 rows x 128 bytes for each of the four output warps
-    static constexpr size_t kSmem = 1024 + kStages * kStageBytes + kOutBytes + 256;
+    static constexpr int kStages = 4;
+    static constexpr int kThreads = 384;
+    static constexpr int kOutBytes = 8 * 2 * 4096;                 // two pieces of 32 rows x 128 bytes for each of the eight output warps
+    static constexpr size_t kSmem = 1024 + kStages * kStageBytes + kOutBytes + 256 + 8 * 64 * 4;
 };
 
 struct GemmParams {
@@ -73,7 +73,8 @@ struct GemmParams {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, const GemmParams p)
+__global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
+                                                                       const __grid_constant__ CUtensorMap tmO, const GemmParams p)
 {
     using C = GemmCfg;
     constexpr int kS = C::kStages;
@@ -88,7 +89,7 @@ __global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
         for (int s = 0; s < kS; ++s) mbar_init(smem_u32(full + s), 1), mbar_init(smem_u32(empty + s), 1);
-        for (int b = 0; b < 2; ++b) mbar_init(smem_u32(acc_full + b), 1), mbar_init(smem_u32(acc_empty + b), 4);
+        for (int b = 0; b < 2; ++b) mbar_init(smem_u32(acc_full + b), 1), mbar_init(smem_u32(acc_empty + b), 8);
         *abort_flag = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -158,79 +159,89 @@ __global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_
         }
         __syncwarp();
     } else if (warp >= 4) {
-        constexpr int kCols = 128 / (int)sizeof(T);   // columns of a 128-byte piece of a row
-        constexpr int kPiece = kCols;
-        const int w = warp - 4;
-        unsigned char *stg = smOut + w * 4096;
-        int t = 0;
+        // Two warps to a quarter of the rows, each with half of the columns: pieces of 128 bytes of a row, swizzled in shared memory so that the
+        // lanes (one row each) stay on different banks and a tile store takes them in the same form.
+        constexpr int kCols = 128 / (int)sizeof(T);   // columns of a piece
+        const int w = (warp - 4) & 3, half = (warp - 4) >> 2;
+        unsigned char *stg = smOut + (warp - 4) * 2 * 4096;
+        float *bias_s = reinterpret_cast<float *>(smOut + C::kOutBytes + 256) + (warp - 4) * 64;
+        int t = 0, slab = 0;
         for (int64_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, ++t) {
             const int b = t & 1;
+            const int64_t row0 = tile / p.n_tiles * kBM + w * 32;
+            const int n0 = (int)(tile % p.n_tiles) * kBN + half * 64;
+            __syncwarp();
+#pragma unroll
+            for (int x = 0; x < 64; x += 32) bias_s[x + lane] = p.bias && n0 + x + lane < p.n ? __ldg(p.bias + n0 + x + lane) : 0.f;
+            __syncwarp();
             if (!mbar_wait(smem_u32(acc_full + b), (uint32_t)((t >> 1) & 1), abort_flag)) break;
             tc_fence_after();
-            const int64_t row0 = tile / p.n_tiles * kBM + w * 32;
-            const int n0 = (int)(tile % p.n_tiles) * kBN;
-#pragma unroll 1
-            for (int c0 = 0; c0 < kBN; c0 += kPiece) {
+            uint32_t r[64];
+            const uint32_t src = tmem + ((uint32_t)(w * 32) << 16) + (uint32_t)(b * 128 + half * 64);
+            tmem_ld32(src, *reinterpret_cast<uint32_t(*)[32]>(&r[0]));
+            tmem_ld32(src + 32, *reinterpret_cast<uint32_t(*)[32]>(&r[32]));
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(acc_empty + b));   // in registers: the accumulator is free
+#pragma unroll
+            for (int c0 = 0; c0 < 64; c0 += kCols) {
                 const int col = n0 + c0;
-#pragma unroll
-                for (int h = 0; h < kPiece; h += 32) {
-                    uint32_t r[32];
-                    tmem_ld32(tmem + ((uint32_t)(w * 32) << 16) + (uint32_t)(b * 128 + c0 + h), r);
-                    tmem_ld_wait();
-                    if (c0 + h + 32 == kBN) {   // all of it is in registers: the accumulator is free
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(acc_empty + b));
-                    }
-                    float v[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        v[i] = __uint_as_float(r[i]);
-                        if (p.bias) v[i] += col + h + i < p.n ? __ldg(p.bias + col + h + i) : 0.f;
-                        if (p.relu) v[i] = v[i] < 0.f ? 0.f : v[i];   // NaN stays
-                    }
-                    // 16-byte pieces of the row, in an order that keeps the lanes (one row each) on different banks
-#pragma unroll
-                    for (int q = 0; q < 32 * (int)sizeof(T) / 16; ++q) {
-                        uint4 o;
-                        if constexpr (sizeof(T) == 2) {
-                            uint32_t pk[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const __nv_bfloat162 hh = __floats2bfloat162_rn(v[8 * q + 2 * i], v[8 * q + 2 * i + 1]);
-                                pk[i] = *reinterpret_cast<const uint32_t *>(&hh);
-                            }
-                            o = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-                        } else {
-                            o = make_uint4(__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3]));
-                        }
-                        const int piece = h * (int)sizeof(T) / 16 + q;
-                        *reinterpret_cast<uint4 *>(stg + lane * 128 + ((piece ^ (lane & 7)) << 4)) = o;
-                    }
-                }
+                if (col >= p.n) break;
+                unsigned char *sb = stg + slab * 4096;
+                if (p.wide && lane == 0) bulk_wait_read<1>();   // the store that last read this slab is done with it
                 __syncwarp();
-                T *out = static_cast<T *>(p.out);
-                constexpr int kPer = 16 / (int)sizeof(T);          // elements of a 16-byte piece
-                constexpr int kLanes = kPiece * (int)sizeof(T) / 16;   // lanes to a row
-                const int lr = lane / kLanes, lp = lane % kLanes;
+                constexpr int kPer = 16 / (int)sizeof(T);       // elements of 16 bytes
 #pragma unroll
-                for (int i = 0; i < kLanes; ++i) {
-                    const int r = i * (32 / kLanes) + lr;
-                    const int64_t row = row0 + r;
-                    const uint4 o = *reinterpret_cast<const uint4 *>(stg + r * 128 + ((lp ^ (r & 7)) << 4));
-                    const int c = col + lp * kPer;
-                    if (row < p.m && c < p.n) {
-                        T *dst = out + row * p.out_stride + c;
-                        if (p.wide && c + kPer <= p.n) *reinterpret_cast<uint4 *>(dst) = o;
-                        else {
-                            const T *e = reinterpret_cast<const T *>(&o);
-                            for (int x = 0; x < kPer && c + x < p.n; ++x) dst[x] = e[x];
+                for (int q = 0; q < 8; ++q) {
+                    float v[kPer];
+#pragma unroll
+                    for (int i = 0; i < kPer; i += 4) {
+                        const float4 bb = *reinterpret_cast<const float4 *>(bias_s + c0 + q * kPer + i);
+                        const float add[4] = {bb.x, bb.y, bb.z, bb.w};
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) {
+                            v[i + x] = __uint_as_float(r[c0 + q * kPer + i + x]) + add[x];
+                            if (p.relu) v[i + x] = v[i + x] < 0.f ? 0.f : v[i + x];   // NaN stays
                         }
                     }
+                    uint4 o;
+                    if constexpr (sizeof(T) == 2) {
+                        uint32_t pk[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const __nv_bfloat162 hh = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                            pk[i] = *reinterpret_cast<const uint32_t *>(&hh);
+                        }
+                        o = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+                    } else {
+                        o = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                    }
+                    *reinterpret_cast<uint4 *>(sb + lane * 128 + ((q ^ (lane & 7)) << 4)) = o;
                 }
-                __syncwarp();
+                if (p.wide) {
+                    // rows and columns behind the end are not stored
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (row0 < p.m) tma_store_2d(&tmO, smem_u32(sb), col, (int)row0);
+                        bulk_commit();
+                    }
+                    slab ^= 1;
+                } else {
+                    __syncwarp();
+                    // a row at a time, a lane to an element
+                    T *out = static_cast<T *>(p.out);
+                    for (int rr = 0; rr < 32 && row0 + rr < p.m; ++rr) {
+#pragma unroll
+                        for (int x = lane; x < kCols; x += 32)
+                            if (col + x < p.n) out[(row0 + rr) * p.out_stride + col + x] = *reinterpret_cast<const T *>(sb + rr * 128 + ((x / kPer ^ (rr & 7)) << 4) + x % kPer * sizeof(T));
+                    }
+                    __syncwarp();
+                }
             }
         }
+        if (lane == 0) bulk_wait<0>();   // all stores of this warp have reached global memory
     }
 
     if (*abort_flag) {
@@ -261,16 +272,26 @@ template <typename T>
 cudaError_t run_gemm(GemmParams p, const uint8_t *a_codes, const uint8_t *w_codes, cudaStream_t st)
 {
     using C = GemmCfg;
-    CUtensorMap ta, tw;
+    CUtensorMap ta, tw, to{};
     cudaError_t e = encode_codes(&ta, a_codes, p.m, p.k, kBM);
     if (e == cudaSuccess) e = encode_codes(&tw, w_codes, p.n, p.k, kBN);
+    if (e == cudaSuccess && p.wide) {
+        // the output as it is stored: 128-byte pieces of 32 rows
+        const cuuint64_t dims[2] = {(cuuint64_t)p.n, (cuuint64_t)p.m};
+        const cuuint64_t strides[1] = {(cuuint64_t)(p.out_stride * sizeof(T))};
+        const cuuint32_t box[2] = {(cuuint32_t)(128 / sizeof(T)), 32};
+        const cuuint32_t estr[2] = {1, 1};
+        const CUresult r = encode_fn()(&to, sizeof(T) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, p.out, dims, strides, box, estr,
+                                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        if (r != CUDA_SUCCESS) e = cudaErrorInvalidValue;
+    }
     // (an attribute of the device's copy of the kernel: set for whichever device is current)
     if (e == cudaSuccess) e = cudaFuncSetAttribute(k_mx4_gemm<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
     if (e != cudaSuccess) return e;
     p.n_tiles = (p.n + kBN - 1) / kBN;
     p.tiles = (p.m + kBM - 1) / kBM * p.n_tiles;
     const unsigned grid = (unsigned)(p.tiles < 148 ? p.tiles : 148);
-    e = launch_pdl(k_mx4_gemm<T>, dim3(grid), dim3(C::kThreads), C::kSmem, st, ta, tw, p);
+    e = launch_pdl(k_mx4_gemm<T>, dim3(grid), dim3(C::kThreads), C::kSmem, st, ta, tw, to, p);
     count_launch();
     return e;
 }
