@@ -26,21 +26,30 @@ __host__ __device__ constexpr uint32_t umma_idesc_mxf4(int m, int n, int pair)
 {
     return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | ((uint32_t)(m >> 4) << 24) | ((uint32_t)pair << 29) | ((uint32_t)pair << 4);
 }
-__device__ __forceinline__ void umma_mxf4(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t a_scale, uint32_t b_scale, uint32_t accumulate)
+// (the whole warp walks and the lane with `one` set issues: see umma_bf16_if)
+__device__ __forceinline__ void umma_mxf4(uint32_t one, uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t a_scale, uint32_t b_scale, uint32_t accumulate)
 {
     asm volatile(
         "{\n"
-        ".reg .pred p;\n"
+        ".reg .pred p, q;\n"
         "setp.ne.b32 p, %6, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n"
+        "setp.ne.b32 q, %7, 0;\n"
+        "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n"
         "}\n" ::"r"(d_tmem),
-        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate)
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(a_scale), "r"(b_scale), "r"(accumulate), "r"(one)
         : "memory");
 }
 // 512 bytes (32 rows x 16 bytes) to four tensor-memory columns, the same in every quarter of the lanes.
-__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc)
+__device__ __forceinline__ void tmem_copy_scales(uint32_t one, uint32_t taddr, uint64_t desc)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    asm volatile(
+        "{\n"
+        ".reg .pred q;\n"
+        "setp.ne.b32 q, %2, 0;\n"
+        "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n"
+        "}\n" ::"r"(taddr),
+        "l"(desc), "r"(one)
+        : "memory");
 }
 
 constexpr int kBM = 128;
@@ -128,36 +137,40 @@ __global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
-            uint32_t it = 0;
-            int t = 0;
-            bool ok = true;
-            for (int64_t tile = blockIdx.x; ok && tile < p.tiles; tile += gridDim.x, ++t) {
-                const int b = t & 1;
-                if (t >= 2 && !mbar_wait(smem_u32(acc_empty + b), (uint32_t)(((t - 2) >> 1) & 1), abort_flag)) break;
-                for (int j = 0; j < stages; ++j, ++it) {
-                    const int s = (int)(it % kS);
-                    if (!mbar_wait(smem_u32(full + s), (it / kS) & 1u, abort_flag)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    const int steps = min(4, (p.k - j * kStageK + 63) / 64);   // products of 64 k; codes behind the last column are zero
-                    const uint32_t sc_t = tmem + (uint32_t)(kTmemScales + s * 16);
-                    for (int h = 0; 2 * h < steps; ++h) {
-                        tmem_copy_scales(sc_t + 4 * h, umma_desc_plain(smem_u32(smSc + s * 2048 + h * 512), 16));
-                        tmem_copy_scales(sc_t + 8 + 4 * h, umma_desc_plain(smem_u32(smSc + s * 2048 + 1024 + h * 512), 16));
-                    }
-                    const uint64_t ad = umma_desc_sw128(smem_u32(smA + s * C::kABytes)), bd = umma_desc_sw128(smem_u32(smB + s * C::kBBytes));
-                    for (int q = 0; q < steps; ++q)
-                        umma_mxf4(tmem + (uint32_t)(b * 128), ad + 2 * q, bd + 2 * q, umma_idesc_mxf4(kBM, kBN, (q & 1) * 2), sc_t + 4 * (q >> 1),
-                                  sc_t + 8 + 4 * (q >> 1), j > 0 || q > 0);
-                    umma_commit(smem_u32(empty + s));
+        const uint32_t one = elect_one();
+        const uint64_t ad0 = umma_desc_sw128(smem_u32(smA)), bd0 = umma_desc_sw128(smem_u32(smB)), sd0 = umma_desc_plain(smem_u32(smSc), 16);
+        uint32_t it = 0;
+        int t = 0;
+        bool ok = true;
+        for (int64_t tile = blockIdx.x; ok && tile < p.tiles; tile += gridDim.x, ++t) {
+            const int b = t & 1;
+            if (t >= 2 && !mbar_wait(smem_u32(acc_empty + b), (uint32_t)(((t - 2) >> 1) & 1), abort_flag)) break;
+            for (int j = 0; j < stages; ++j, ++it) {
+                const uint32_t s = it % kS;
+                if (!mbar_wait(smem_u32(full + s), (it / kS) & 1u, abort_flag)) {
+                    ok = false;
+                    break;
                 }
-                if (ok) umma_commit(smem_u32(acc_full + b));
+                tc_fence_after();
+                const int steps = min(4, (p.k - j * kStageK + 63) / 64);   // products of 64 k; codes behind the last column are zero
+                const uint32_t sc_t = tmem + (uint32_t)(kTmemScales + s * 16);
+                const uint64_t ad = ad0 + (uint64_t)(s * (C::kABytes >> 4)), bd = bd0 + (uint64_t)(s * (C::kBBytes >> 4)), sd = sd0 + (uint64_t)(s * (2048 >> 4));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (2 * h >= steps) break;
+                    tmem_copy_scales(one, sc_t + 4 * h, sd + (uint64_t)(h * (512 >> 4)));
+                    tmem_copy_scales(one, sc_t + 8 + 4 * h, sd + (uint64_t)((1024 + h * 512) >> 4));
+                }
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (q >= steps) break;
+                    umma_mxf4(one, tmem + (uint32_t)(b * 128), ad + 2 * q, bd + 2 * q, umma_idesc_mxf4(kBM, kBN, (q & 1) * 2), sc_t + 4 * (q >> 1), sc_t + 8 + 4 * (q >> 1),
+                              j > 0 || q > 0);
+                }
+                umma_commit_if(one, smem_u32(empty + s));
             }
+            if (ok) umma_commit_if(one, smem_u32(acc_full + b));
         }
-        __syncwarp();
     } else if (warp >= 4) {
         // Two warps to a quarter of the rows, each with half of the columns: pieces of 128 bytes of a row, swizzled in shared memory so that the
         // lanes (one row each) stay on different banks and a tile store takes them in the same form.
