@@ -312,7 +312,20 @@ __device__ __forceinline__ int entry_of(const int64_t *offsets, int n, int64_t r
     return lo;
 }
 
-constexpr int kRowSlices = 4;   // slices of 32 lanes x 8 elements that a warp has in flight
+// A CTA of the row kernels takes whole rows, about kRowItems pieces of eight elements; 32-bit divisions by a fixed number are a multiplication.
+constexpr int kRowItems = 1024, kRowThreads = 256, kMostRows = kRowItems / 4;   // (a row has four pieces at least)
+struct FastDiv {
+    uint32_t by, mul, shift;   // x / by = (x mul) >> (32 + shift), x < 2^24
+    static FastDiv of(uint32_t by)
+    {
+        FastDiv f{by, 0u, 0u};
+        while ((1u << f.shift) < by) ++f.shift;
+        f.mul = (uint32_t)(((uint64_t)1 << 32) * ((1ull << f.shift) - by) / by + 1);   // round-up multiplier less 2^32
+        return f;
+    }
+    __device__ uint32_t div(uint32_t x) const { return (uint32_t)(((uint64_t)__umulhi(x, mul) + x) >> shift); }
+};
+inline int rows_of_cta(int per_row) { return std::max(1, kRowItems / per_row); }
 
 struct AppendParams {
     Cache4 c;
@@ -322,15 +335,19 @@ struct AppendParams {
     const void *x[2];
     int64_t rows, stride;
     int32_t row_blocks;   // CTAs that bring rows; the ones behind them copy shared last pages
+    int32_t cta_rows;
+    FastDiv per_row, per_head;   // pieces of eight elements of a row, of a head's row
 };
 
-// Rows to pages: four lanes quantise a block of 32 elements, so a warp reads 512 (bf16) consecutive bytes at a time.
+// Rows to pages: four lanes quantise a block of 32 elements, so a warp reads 512 (bf16) consecutive bytes at a time; where a row goes is looked up once,
+// while its elements are on their way.
 template <typename T, bool ALIGNED>
-__global__ void __launch_bounds__(256) k_append(const AppendParams p)
+__global__ void __launch_bounds__(kRowThreads) k_append(const AppendParams p)
 {
     const Cache4 &c = p.c;
     const Scratch s = scratch_of(c);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = blockIdx.y;
+    __shared__ int64_t place[kMostRows];   // row of a page (of head 0) that a row of the CTA goes to, or -1
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, which = blockIdx.y;
     if ((int)blockIdx.x >= p.row_blocks) {
         // the rows that a copied last page held: codes in 16-byte pieces, scale bytes one by one (the rows behind them are being written)
         for (int i = ((int)blockIdx.x - p.row_blocks) * 8 + warp; i < p.n; i += (gridDim.x - p.row_blocks) * 8) {
@@ -349,39 +366,46 @@ __global__ void __launch_bounds__(256) k_append(const AppendParams p)
         }
         return;
     }
-    const int per_row = c.heads * c.d / 8;   // lanes to a row
-    const int64_t all = min(p.offsets[p.n], p.rows) * per_row;
-    const int64_t g0 = ((int64_t)blockIdx.x * 8 + warp) * (kRowSlices * 32);
-    if (g0 >= all) return;
-    float v[kRowSlices][8];
-    int64_t row[kRowSlices];
-    int part[kRowSlices];
+    const int64_t row0 = (int64_t)blockIdx.x * p.cta_rows, all = min(p.offsets[p.n], p.rows);
+    const int rows = (int)min((int64_t)p.cta_rows, all - row0), items = rows * (int)p.per_row.by;
+    if (rows <= 0) return;
+    const T *x = static_cast<const T *>(p.x[which]) + row0 * p.stride;
+    for (int i0 = 0; i0 < items; i0 += 4 * kRowThreads) {
+        Raw8<T> v[4];
+        int row[4], part[4];
 #pragma unroll
-    for (int u = 0; u < kRowSlices; ++u) {
-        const int64_t g = g0 + u * 32 + lane;
-        row[u] = g / per_row, part[u] = (int)(g - row[u] * per_row);
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * kRowThreads + tid;
+            row[u] = (int)p.per_row.div((uint32_t)i), part[u] = i - row[u] * (int)p.per_row.by;
+            v[u] = Raw8<T>{};
+            if (i < items) v[u] = load_raw8<T, ALIGNED>(x + row[u] * p.stride + part[u] * 8);
+        }
+        if (i0 == 0) {
+            if (tid < rows) {
+                const int64_t r = row0 + tid;
+                int64_t to = -1;
+                if (r >= p.offsets[0]) {
+                    const int e = entry_of(p.offsets, p.n, r), first = s.info[e];
+                    if (first >= 0) {   // (offsets ascend then)
+                        const int at = first + (int)(r - p.offsets[e]);
+                        const int page = c.table[(size_t)p.seq_ids[e] * c.max_pages + (at >> c.page_shift)];
+                        if (c.holds(page)) to = (int64_t)c.row(page, 0, at & (c.page_rows() - 1));
+                    }
+                }
+                place[tid] = to;
+            }
+            __syncthreads();
+        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[u][e] = 0.f;
-        if (g < all) load8<T, ALIGNED>(static_cast<const T *>(p.x[which]) + row[u] * p.stride + part[u] * 8, v[u]);
-    }
-    int e = -1;
-#pragma unroll
-    for (int u = 0; u < kRowSlices; ++u) {
-        uint32_t byte;
-        const uint32_t w = mx_quantise_quad(v[u], byte);
-        if (g0 + u * 32 + lane >= all) continue;
-        if (row[u] < __ldg(p.offsets)) continue;
-        if (e < 0) e = entry_of(p.offsets, p.n, row[u]);
-        while (row[u] >= __ldg(p.offsets + e + 1)) ++e;
-        const int first = s.info[e];
-        if (first < 0) continue;
-        const int at = first + (int)(row[u] - __ldg(p.offsets + e));
-        const int page = c.table[(size_t)p.seq_ids[e] * c.max_pages + (at >> c.page_shift)];
-        if (!c.holds(page)) continue;
-        const int head = part[u] / (c.d / 8), sub = part[u] - head * (c.d / 8);
-        const size_t r = c.row(page, head, at & (c.page_rows() - 1));
-        reinterpret_cast<uint32_t *>(c.codes[which] + r * (c.d / 2))[sub] = w;
-        if ((sub & 3) == 0) c.scales[which][r * (c.d / 32) + (sub >> 2)] = (uint8_t)byte;
+        for (int u = 0; u < 4; ++u) {
+            uint32_t byte;
+            const uint32_t w = mx_quantise_quad<T>(v[u], byte);
+            if (i0 + u * kRowThreads + tid >= items || place[row[u]] < 0) continue;
+            const int head = (int)p.per_head.div((uint32_t)part[u]), sub = part[u] - head * (int)p.per_head.by;
+            const size_t r = (size_t)place[row[u]] + ((size_t)head << c.page_shift);
+            reinterpret_cast<uint32_t *>(c.codes[which] + r * (c.d / 2))[sub] = w;
+            if ((sub & 3) == 0) c.scales[which][r * (c.d / 32) + (sub >> 2)] = (uint8_t)byte;
+        }
     }
 }
 
@@ -392,59 +416,66 @@ struct ReadParams {
     const int64_t *offsets;
     void *out[2];
     int64_t rows, stride;
+    int32_t cta_rows;
+    FastDiv per_row, per_head;
 };
 
 template <typename T, bool ALIGNED>
-__global__ void __launch_bounds__(256) k_read(const ReadParams p)
+__global__ void __launch_bounds__(kRowThreads) k_read(const ReadParams p)
 {
     const Cache4 &c = p.c;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = blockIdx.y;
+    __shared__ int64_t place[kMostRows];   // row of a page (of head 0); -1: nobody's row; -2: a row that is not there
+    const int tid = threadIdx.x, which = blockIdx.y;
     bool bad = false;
-    for (int i = threadIdx.x; i < p.n; i += 256) {
+    for (int i = tid; i < p.n; i += kRowThreads) {
         const int64_t a = p.offsets[i], b = p.offsets[i + 1];
         bad |= a < 0 || b < a || b > p.rows;
     }
     if (__syncthreads_or(bad)) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(c.status, AIF_STATUS_BAD_ID);
+        if (blockIdx.x == 0 && tid == 0) atomicOr(c.status, AIF_STATUS_BAD_ID);
         return;
     }
-    const int per_row = c.heads * c.d / 8;
-    const int64_t all = p.offsets[p.n] * per_row;
-    const int64_t g0 = ((int64_t)blockIdx.x * 8 + warp) * (kRowSlices * 32);
-    if (g0 >= all) return;
-    uint32_t w[kRowSlices];
-    float scale[kRowSlices];
-    int e = -1;
-    bool missing = false;
-#pragma unroll
-    for (int u = 0; u < kRowSlices; ++u) {
-        w[u] = 0u, scale[u] = 0.f;
-        const int64_t g = g0 + u * 32 + lane, row = g / per_row;
-        if (g >= all || row < __ldg(p.offsets)) continue;
-        if (e < 0) e = entry_of(p.offsets, p.n, row);
-        while (row >= __ldg(p.offsets + e + 1)) ++e;
-        const int part = (int)(g - row * per_row), head = part / (c.d / 8), sub = part - head * (c.d / 8);
-        const int q = p.seq_ids[e];
-        const int64_t at = row - __ldg(p.offsets + e);
-        int page = -1;
-        if (q >= 0 && q < c.n_seqs && at < c.lengths[q] && at < c.longest()) page = c.table[(size_t)q * c.max_pages + (at >> c.page_shift)];
-        if (!c.holds(page)) {
-            missing = true;
-            continue;
+    const int64_t row0 = (int64_t)blockIdx.x * p.cta_rows;
+    const int rows = (int)min((int64_t)p.cta_rows, p.offsets[p.n] - row0), items = rows * (int)p.per_row.by;
+    if (rows <= 0) return;
+    if (tid < rows) {
+        const int64_t r = row0 + tid;
+        int64_t from = -1;
+        if (r >= p.offsets[0]) {
+            const int e = entry_of(p.offsets, p.n, r), q = p.seq_ids[e];
+            const int64_t at = r - p.offsets[e];
+            int page = -1;
+            if (q >= 0 && q < c.n_seqs && at < c.lengths[q] && at < c.longest()) page = c.table[(size_t)q * c.max_pages + (at >> c.page_shift)];
+            from = c.holds(page) ? (int64_t)c.row(page, 0, (int)at & (c.page_rows() - 1)) : -2;
+            if (from == -2) atomicOr(c.status, AIF_STATUS_BAD_ID);
         }
-        const size_t r = c.row(page, head, (int)at & (c.page_rows() - 1));
-        w[u] = __ldg(reinterpret_cast<const uint32_t *>(c.codes[which] + r * (c.d / 2)) + sub);
-        scale[u] = mx_scale(__ldg(c.scales[which] + r * (c.d / 32) + (sub >> 2)));
+        place[tid] = from;
     }
+    __syncthreads();
+    T *out = static_cast<T *>(p.out[which]) + row0 * p.stride;
+    for (int i0 = 0; i0 < items; i0 += 4 * kRowThreads) {
+        uint32_t w[4], byte[4];
+        int row[4], part[4];
 #pragma unroll
-    for (int u = 0; u < kRowSlices; ++u) {
-        const int64_t g = g0 + u * 32 + lane, row = g / per_row;
-        if (g >= all || row < __ldg(p.offsets)) continue;
-        float v[8];
-        mx_values8(w[u], scale[u], v);
-        store8<T, ALIGNED>(static_cast<T *>(p.out[which]) + row * p.stride + (g - row * per_row) * 8, v);
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * kRowThreads + tid;
+            row[u] = (int)p.per_row.div((uint32_t)i), part[u] = i - row[u] * (int)p.per_row.by;
+            w[u] = 0u, byte[u] = 0u;
+            if (i < items && place[row[u]] >= 0) {
+                const int head = (int)p.per_head.div((uint32_t)part[u]), sub = part[u] - head * (int)p.per_head.by;
+                const size_t r = (size_t)place[row[u]] + ((size_t)head << c.page_shift);
+                w[u] = __ldg(reinterpret_cast<const uint32_t *>(c.codes[which] + r * (c.d / 2)) + sub);
+                byte[u] = __ldg(c.scales[which] + r * (c.d / 32) + (sub >> 2));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (i0 + u * kRowThreads + tid >= items || place[row[u]] == -1) continue;
+            float v[8];
+            mx_values8(w[u], mx_scale(byte[u]), v);
+            store8<T, ALIGNED>(out + row[u] * p.stride + part[u] * 8, v);
+        }
     }
-    if (__any_sync(__activemask(), missing) && missing) atomicOr(c.status, AIF_STATUS_BAD_ID);
 }
 
 // ---- whole pages ------------------------------------------------------------------------------------------------
@@ -603,8 +634,7 @@ int check_rows(const aif_cache4 *c, const void *k, const void *v, int32_t dtype,
 {
     if (dtype != AIF_F32 && dtype != AIF_BF16) return AIF_ERR_ARG;
     if (rows < 0 || rows > (int64_t)1 << 40 || stride < (int64_t)c->heads * c->d || stride > (int64_t)1 << 31) return AIF_ERR_SHAPE;
-    // a warp of the row kernels takes 4 x 32 x 8 elements
-    if (rows * (c->heads * c->d / 8) / (kRowSlices * 256) > INT_MAX - 2 - c->n_seqs) return AIF_ERR_SHAPE;
+    if (rows / rows_of_cta(c->heads * c->d / 8) > INT_MAX - 1024) return AIF_ERR_SHAPE;   // CTAs of a grid
     const unsigned el = dtype == AIF_BF16 ? 2 : 4;
     if ((c->shared != 0) != (v == nullptr)) return AIF_ERR_ARG;
     if (rows > 0 && (!k || reinterpret_cast<uintptr_t>(k) % el != 0 || (v && reinterpret_cast<uintptr_t>(v) % el != 0))) return AIF_ERR_ARG;
@@ -697,11 +727,12 @@ int aif_cache4_append(const aif_cache4 *c, int32_t n, const int32_t *seq_ids, co
     if (e == cudaSuccess && rows > 0) {
         AppendParams p{};
         p.c = b.c, p.n = n, p.seq_ids = seq_ids, p.offsets = offsets, p.x[0] = k, p.x[1] = v, p.rows = rows, p.stride = stride;
-        p.row_blocks = (int)grid_for(rows * (c->heads * c->d / 8), kRowSlices * 256, INT_MAX);
+        p.per_row = FastDiv::of(c->heads * c->d / 8), p.per_head = FastDiv::of(c->d / 8), p.cta_rows = rows_of_cta(c->heads * c->d / 8);
+        p.row_blocks = (int)grid_for(rows, p.cta_rows, INT_MAX);
         const dim3 grid((unsigned)p.row_blocks + grid_for(n, 8, 148), c->shared ? 1 : 2);
         const int el = dtype == AIF_BF16 ? 2 : 4;
         const bool al = at16(k) && at16(v) && stride * el % 16 == 0;
-        auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(p); };
+        auto go = [&](auto kernel) { kernel<<<grid, kRowThreads, 0, st>>>(p); };
         if (dtype == AIF_BF16) al ? go(k_append<__nv_bfloat16, true>) : go(k_append<__nv_bfloat16, false>);
         else al ? go(k_append<float, true>) : go(k_append<float, false>);
         count_launch();
@@ -766,10 +797,11 @@ int aif_cache4_read(const aif_cache4 *c, int32_t n, const int32_t *seq_ids, cons
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     ReadParams p{};
     p.c = cache4_of(c), p.n = n, p.seq_ids = seq_ids, p.offsets = offsets, p.out[0] = k_out, p.out[1] = v_out, p.rows = rows, p.stride = stride;
-    const dim3 grid(grid_for(rows * (c->heads * c->d / 8), kRowSlices * 256, INT_MAX), c->shared ? 1 : 2);
+    p.per_row = FastDiv::of(c->heads * c->d / 8), p.per_head = FastDiv::of(c->d / 8), p.cta_rows = rows_of_cta(c->heads * c->d / 8);
+    const dim3 grid(grid_for(rows, p.cta_rows, INT_MAX), c->shared ? 1 : 2);
     const int el = dtype == AIF_BF16 ? 2 : 4;
     const bool al = at16(k_out) && at16(v_out) && stride * el % 16 == 0;
-    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(p); };
+    auto go = [&](auto kernel) { kernel<<<grid, kRowThreads, 0, st>>>(p); };
     if (dtype == AIF_BF16) al ? go(k_read<__nv_bfloat16, true>) : go(k_read<__nv_bfloat16, false>);
     else al ? go(k_read<float, true>) : go(k_read<float, false>);
     count_launch();

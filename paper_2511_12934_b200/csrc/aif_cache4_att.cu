@@ -262,31 +262,76 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_att4_rows(const AttCall a)
     if (bad_page) atomicOr(c.status, AIF_STATUS_BAD_ID);
 }
 
-// Tiles that were cut, one per CTA of the attention kernel at most: sums of the pieces, brought to one offset, over their weights.
-// The rows of a tile are spread over gridDim.y CTAs.
+// Tiles that were cut, one per CTA of the attention kernel at most: sums of the pieces, brought to one offset, over their weights.  Block (c, y) has eight
+// rows of the tile that ended in CTA c, a warp to a row; where a tile has fewer rows, several warps share the pieces of one.
+constexpr int kJoinPieces = 448;   // most CTAs of an attention kernel, so most pieces of a tile
 template <typename T>
 __global__ void __launch_bounds__(256) k_att4_join(const AttCall a, int permuted)
 {
     grid_dep_wait();
     grid_dep_launch();
     const PieceHeader h = a.headers[blockIdx.x];
-    if (h.first_cta < 0) return;
-    const int d = a.c.d, last = blockIdx.x;
+    const int first_row = blockIdx.y * 8;
+    if (h.first_cta < 0 || first_row >= h.rows) return;
+    __shared__ float factor[8][kJoinPieces];
+    __shared__ float4 part_sum[8][32];
+    const int d = a.c.d, pieces = (int)blockIdx.x - h.first_cta + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rows = min(8, h.rows - first_row);
+    int share = 1;   // warps to a row
+    while (share * 2 * rows <= 8) share *= 2;
+    const int r = first_row + warp / share, part = warp % share;
+    const bool work = warp < rows * share;
     const size_t record = (size_t)a.tile_rows * (d + 2);
-    for (int x = blockIdx.y * 256 + threadIdx.x; x < h.rows * d; x += gridDim.y * 256) {
-        const int r = x / d, col = x - r * d;
+    // the piece of CTA first_cta is the beginning of a tile, the others are continuations
+    auto piece = [&](int p) { return a.records + (size_t)(2 * (h.first_cta + p) + (p == 0)) * record; };
+    float weight = 0.f;
+    if (work) {
         float mt = -FLT_MAX;
-        for (int p = h.first_cta; p <= last; ++p) mt = fmaxf(mt, a.records[(2 * p + (p == h.first_cta)) * record + (size_t)a.tile_rows * d + 2 * r]);
-        float sum = 0.f, weight = 0.f;
-        for (int p = h.first_cta; p <= last; ++p) {
-            const float *rec = a.records + (2 * p + (p == h.first_cta)) * record;
-            const float f = fast_exp2(rec[(size_t)a.tile_rows * d + 2 * r] - mt);
-            // the tensor-core kernel's sums stand in the order of the unpacked codes: 0, 4, 1, 5, 2, 6, 3, 7
-            const int at = permuted ? (col & ~7) | ((col & 3) << 1) | ((col >> 2) & 1) : col;
-            sum += rec[r * d + at] * f, weight += rec[(size_t)a.tile_rows * d + 2 * r + 1] * f;
+        for (int p = lane; p < pieces; p += 32) mt = fmaxf(mt, piece(p)[(size_t)a.tile_rows * d + 2 * r]);
+#pragma unroll
+        for (int b = 16; b > 0; b >>= 1) mt = fmaxf(mt, __shfl_xor_sync(0xffffffffu, mt, b));
+        for (int p = lane; p < pieces; p += 32) {
+            const float *st = piece(p) + (size_t)a.tile_rows * d + 2 * r;
+            const float f = fast_exp2(st[0] - mt);
+            factor[warp][p] = f, weight += st[1] * f;
         }
-        const int rr = h.r0 + r, query = rr / a.group;
-        static_cast<T *>(a.out)[(h.row0 + query) * a.out_stride + (h.head * a.group + rr - query * a.group) * d + col] = (T)(sum / weight);
+#pragma unroll
+        for (int b = 16; b > 0; b >>= 1) weight += __shfl_xor_sync(0xffffffffu, weight, b);
+    }
+    __syncwarp();
+#pragma unroll 1
+    for (int col0 = 0; col0 < d; col0 += 128) {
+        const int col = col0 + lane * 4;   // of the records: the tensor-core kernels' sums stand in the order of the unpacked codes
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (work && col < d) {
+#pragma unroll 4
+            for (int p = part; p < pieces; p += share) {
+                const float2 x = *reinterpret_cast<const float2 *>(piece(p) + (size_t)r * d + col), y = *reinterpret_cast<const float2 *>(piece(p) + (size_t)r * d + col + 2);
+                const float f = factor[warp][p];
+                sum.x += x.x * f, sum.y += x.y * f, sum.z += y.x * f, sum.w += y.y * f;
+            }
+        }
+        if (share > 1) {
+            part_sum[warp][lane] = sum;
+            __syncthreads();
+            if (work && part == 0) {
+                for (int w = 1; w < share; ++w) {
+                    const float4 o = part_sum[warp + w][lane];
+                    sum.x += o.x, sum.y += o.y, sum.z += o.z, sum.w += o.w;
+                }
+            }
+            __syncthreads();
+        }
+        if (work && part == 0 && col < d) {
+            const int rr = h.r0 + r, query = rr / a.group;
+            T *dst = static_cast<T *>(a.out) + (h.row0 + query) * a.out_stride + (h.head * a.group + rr - query * a.group) * d;
+            const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = col + i, to = permuted ? (at & ~7) | ((at & 1) << 2) | ((at >> 1) & 3) : at;   // 0, 4, 1, 5, 2, 6, 3, 7
+                dst[to] = (T)(v[i] / weight);
+            }
+        }
     }
 }
 
@@ -326,7 +371,7 @@ AttForm form_of(const aif_cache4 *c, const aif_cache4_query *q)
     const bool bf = q->dtype == AIF_BF16;
     if (bf && per_seq > 32 && (c->d == 64 || c->d == 128)) return {AttForm::kPair, 256, 64, 148, 4};
     if (bf && per_seq > 32 && c->d == 256) return {AttForm::kTensor, 128, 64, 148, 4};
-    if (bf && per_seq > 2 && (c->d == 32 || c->d == 64 || c->d == 128 || c->d == 256)) return {AttForm::kFew, 8, -32, c->d == 256 ? 148 : 296, 1};
+    if (bf && (c->d == 32 || c->d == 64 || c->d == 128 || c->d == 256)) return {AttForm::kFew, 8, -16, c->d == 256 ? 296 : 444, 1};
     return {AttForm::kRows, per_seq <= 2 ? 1 : 4, -kRowGroups, 444, 1};
 }
 int64_t workspace_of(const AttForm &f, const aif_cache4 *c)
@@ -395,7 +440,7 @@ int aif_cache4_attention(const aif_cache4 *c, const aif_cache4_query *q, aif_str
                : (shared ? run_rows<float, 4, true>(a, f.grid, st) : run_rows<float, 4, false>(a, f.grid, st));
     if (e == cudaSuccess) {
         const bool tensor = f.kernel == AttForm::kPair || f.kernel == AttForm::kTensor;
-        const dim3 grid(f.grid, tensor ? f.tile_rows / 16 : 1);
+        const dim3 grid(f.grid, (f.tile_rows + 7) / 8);
         e = bf ? launch_pdl(k_att4_join<__nv_bfloat16>, grid, dim3(256), 0, st, a, tensor ? 1 : 0) : launch_pdl(k_att4_join<float>, grid, dim3(256), 0, st, a, 0);
         count_launch();
     }

@@ -16,9 +16,9 @@
 namespace aif {
 namespace {
 
-constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
+constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32;
 constexpr int kFewRows = 8;
-constexpr int kFewGroups = 32;    // groups of 16 rows of a unit
+constexpr int kFewGroups = 16;    // groups of 16 rows of a unit
 constexpr float kWeightBias = 7.f;   // weights are 2^7 at the offset and may grow by 2^8
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -74,38 +74,43 @@ __device__ __forceinline__ void load_row(RowCodes<NB> &r, const uint8_t *codes, 
 template <int NB>
 __device__ __forceinline__ uint32_t top_scale(const RowCodes<NB> &r)
 {
-    uint32_t x = r.sc[0];
-    if (NB == 8) x = __vmaxu4(x, r.sc[NB == 8 ? 1 : 0]);
-    if (NB >= 4) x = __vmaxu4(x, x >> 16);
-    if (NB >= 2) x = max(x & 255u, (x >> 8) & 255u);
-    return x;
+    auto of_word = [](uint32_t x) { return max(max(x & 255u, (x >> 8) & 255u), max((x >> 16) & 255u, x >> 24)); };
+    if constexpr (NB == 1) return r.sc[0];
+    if constexpr (NB == 2) return max(r.sc[0] & 255u, r.sc[0] >> 8);
+    if constexpr (NB == 4) return of_word(r.sc[0]);
+    if constexpr (NB == 8) return max(of_word(r.sc[0]), of_word(r.sc[1]));
 }
 // fp16 pair of 2^(byte - top): 0 below 2^-24, NaN for the byte that says so.
 __device__ __forceinline__ uint32_t relative_scale(uint32_t byte, uint32_t top)
 {
     const uint32_t down = top - byte;
-    const uint32_t h = byte == kMxNan ? 0x7fffu : down <= 14u ? (15u - down) << 10 : down <= 24u ? 1u << (24u - down) : 0u;
+    uint32_t h = down <= 14u ? (15u - down) << 10 : (1u << 24) >> min(down, 31u);
+    h = byte == kMxNan ? 0x7fffu : h;
     return h | (h << 16);
 }
-// The quarter row's values over 2^(top - 127): words 4 i .. 4 i + 3 of o are the pairs of code word i.
+// The quarter row's values over 2^(top - 127): words 4 i .. 4 i + 3 of o are the pairs of code word i.  The lane's words t NB .. t NB + NB - 1 of the 4 NB of a row lie in
+// one block of four words, or (NB = 8) in two.
 template <int NB>
 __device__ __forceinline__ void unpack_row(const RowCodes<NB> &r, uint32_t top, int t, uint32_t (&o)[4 * NB])
 {
+    uint32_t f[NB == 8 ? 2 : 1];
+    if constexpr (NB == 8) {
+        const uint32_t sc = (t & 2 ? r.sc[1] : r.sc[0]) >> (16 * (t & 1));
+        f[0] = relative_scale(sc & 255u, top), f[1] = relative_scale((sc >> 8) & 255u, top);
+    } else {
+        f[0] = relative_scale((r.sc[0] >> (8 * (t * NB / 4))) & 255u, top);
+    }
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-        // block of the lane's word i: words t NB .. t NB + NB - 1 of 4 NB, four to a block
-        const int block = NB >= 4 ? t * (NB / 4) + i / 4 : (t * NB + i) >> 2;
-        const uint32_t sc = NB == 8 ? (block & 4 ? r.sc[NB == 8 ? 1 : 0] : r.sc[0]) : r.sc[0];
-        const uint32_t f = relative_scale((sc >> (8 * (block & 3))) & 255u, top);
         uint32_t h[4];
         mx_decode8_f16(r.w[i], h);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[4 * i + k] = mul_f16x2(h[k], f);
+        for (int k = 0; k < 4; ++k) o[4 * i + k] = mul_f16x2(h[k], f[NB == 8 ? i / 4 : 0]);
     }
 }
 
 template <int NB, bool SHARED>
-__global__ void __launch_bounds__(kFewThreads, NB == 8 ? 1 : 2) k_att4_few(const AttCall a)
+__global__ void __launch_bounds__(kFewThreads, NB == 8 ? 2 : 3) k_att4_few(const AttCall a)
 {
     constexpr int D = 32 * NB, KS = 2 * NB;   // steps of 16 columns
     const Cache4 &c = a.c;
@@ -165,28 +170,27 @@ __global__ void __launch_bounds__(kFewThreads, NB == 8 ? 1 : 2) k_att4_few(const
         float m[2] = {-FLT_MAX, -FLT_MAX}, mw[2] = {-FLT_MAX, -FLT_MAX}, l[2] = {0.f, 0.f};   // offsets of the weights' sum and of the values', per row
 
         RowCodes<NB> kn[2][2], vn[SHARED ? 1 : 2][2];   // [group][key g, key g + 8]
+        // a lane's piece of row g of a page's group: from here, page strides and rows further
+        const uint32_t page_codes = (uint32_t)(c.heads << c.page_shift) * (D / 2), page_scales = (uint32_t)(c.heads << c.page_shift) * NB;
+        const size_t head_row = ((size_t)head << c.page_shift) + g;
         auto fetch = [&](int grp) {   // codes of the groups grp and grp + 1
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-                const int gi = grp + x;
-                const int row = gi < sink_groups ? gi << 4 : (gi + rest_group) << 4;
-                int page = -1;
-                if (gi < g1) page = __ldg(table + (row >> c.page_shift));
+                const int gi = min(grp + x, g1 - 1);   // (an odd last one is read twice and used once)
+                const int row = (gi < sink_groups ? gi : gi + rest_group) << 4;
+                int page = __ldg(table + (row >> c.page_shift));
                 const bool ok = c.holds(page);
-                bad_page |= gi < g1 && !ok;
-                const size_t at = ok ? c.row(page, head, (row & (c.page_rows() - 1)) + g) : 0;
+                bad_page |= !ok;
+                page = ok ? page : 0;
+                const size_t at = head_row + (row & (c.page_rows() - 1));
+                const size_t codes = (size_t)(uint32_t)page * page_codes + at * (D / 2), scales = (size_t)(uint32_t)page * page_scales + at * NB;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    if (ok) load_row<NB>(kn[x][h], c.codes[0] + (at + 8 * h) * (D / 2), c.scales[0] + (at + 8 * h) * NB, t);
-                    else {
+                    load_row<NB>(kn[x][h], c.codes[0] + codes + h * 8 * (D / 2), c.scales[0] + scales + h * 8 * NB, t);
+                    if constexpr (!SHARED) load_row<NB>(vn[x][h], c.codes[1] + codes + h * 8 * (D / 2), c.scales[1] + scales + h * 8 * NB, t);
+                    if (!ok) {   // no such page: no number
 #pragma unroll
-                        for (int i = 0; i < NB; ++i) kn[x][h].w[i] = 0u;
-#pragma unroll
-                        for (int i = 0; i < (NB + 3) / 4; ++i) kn[x][h].sc[i] = 0xffffffffu;   // no such page: no number
-                    }
-                    if constexpr (!SHARED) {
-                        if (ok) load_row<NB>(vn[x][h], c.codes[1] + (at + 8 * h) * (D / 2), c.scales[1] + (at + 8 * h) * NB, t);
-                        else vn[x][h] = kn[x][h];
+                        for (int i = 0; i < (NB + 3) / 4; ++i) kn[x][h].sc[i] = NB == 1 ? 0xffu : NB == 2 ? 0xffffu : 0xffffffffu;
                     }
                 }
             }
@@ -211,16 +215,18 @@ __global__ void __launch_bounds__(kFewThreads, NB == 8 ? 1 : 2) k_att4_few(const
                 const int row = (sink ? gi : gi + rest_group) << 4;
                 const int lo = sink ? 0 : e.rest, hi = sink ? e.first : e.length;   // visible rows of the group: [lo, hi)
                 const bool see[2] = {row + g >= lo && row + g < hi, row + g + 8 >= lo && row + g + 8 < hi};
-                // rows that are not visible read as zero, whatever stands there
+                if (row < lo || row + 16 > hi) {
+                    // rows that are not visible have no scale, whatever stands there (codes are finite)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (!see[h]) {
+                    for (int h = 0; h < 2; ++h)
+                        if (!see[h]) {
 #pragma unroll
-                        for (int i = 0; i < NB; ++i) kc[x][h].w[i] = 0u;
-#pragma unroll
-                        for (int i = 0; i < (NB + 3) / 4; ++i) kc[x][h].sc[i] = 0u;
-                        if constexpr (!SHARED) vc[x][h] = kc[x][h];
-                    }
+                            for (int i = 0; i < (NB + 3) / 4; ++i) {
+                                kc[x][h].sc[i] = 0u;
+                                if constexpr (!SHARED) vc[x][h].sc[i] = 0u;
+                            }
+                        }
+                }
                 uint32_t top[2] = {top_scale<NB>(kc[x][0]), top_scale<NB>(kc[x][1])};
                 uint32_t ka[4 * NB], kb[4 * NB];
                 unpack_row<NB>(kc[x][0], top[0], t, ka);

@@ -16,7 +16,7 @@
 // probabilities lose precision with magnitude.
 // Eight codes of a word come apart as the pairs (0,4) (1,5) (2,6) (3,7) with two shifts, two masks and a multiplication each; queries are put
 // into the same order as they are brought, and sums are taken out of it as they are stored.
-// Rounding: probabilities are rounded to bf16 for the product (relative 2^-9 each, the weights' sum is of the unrounded ones), everything else is fp32.
+// Rounding: probabilities are rounded to bf16 for the product (relative 2^-9 each), and their sum is of the rounded ones, everything else is fp32.
 #include <cfloat>
 #include <type_traits>
 
@@ -222,9 +222,10 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
                                     if (c0 + 2 * i >= vc) p0 = 0.f;
                                     if (c0 + 2 * i + 1 >= vc) p1 = 0.f;
                                 }
-                                ls2[i & 1] = add_f32x2(ls2[i & 1], pack_f32x2(p0, p1));
                                 const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
                                 packed[i] = *reinterpret_cast<const uint32_t *>(&h);
+                                // the sum is of the rounded weights, those that the values get: a row with one heavy key is then as exact as its value
+                                ls2[i & 1] = add_f32x2(ls2[i & 1], pack_f32x2(__uint_as_float(packed[i] << 16), __uint_as_float(packed[i] & 0xffff0000u)));
                             }
                             tmem_st16(ts + (uint32_t)(c0 / 2), packed);
                         }

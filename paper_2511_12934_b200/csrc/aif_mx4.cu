@@ -23,17 +23,26 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const T *__restrict__ x, i
     const int t = (int)(blockIdx.x % kt);
     const int tid = threadIdx.x, sub = tid & 15;
     const int col = t * kTile + sub * 8;
+    // four rows of a thread in flight at a time
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = i * 16 + (tid >> 4);
-        const int64_t row = band * kTile + r;
-        const bool in = row < rows && col < cols;   // the four lanes of a block agree: cols is a multiple of 32
-        float v[8] = {};
-        if (in) load8<T, ALIGNED>(x + row * stride + col, v);
-        uint32_t byte;
-        const uint32_t w = mx_quantise_quad(v, byte);
-        if (in) *reinterpret_cast<uint32_t *>(codes + row * (cols / 2) + col / 2) = w;
-        if ((sub & 3) == 0) tile[mx_scale_at(r, sub >> 2)] = (uint8_t)(in ? byte : 0u);   // padding: 2^-127, which times a zero code is nothing
+    for (int i0 = 0; i0 < 8; i0 += 4) {
+        Raw8<T> v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = band * kTile + (i0 + i) * 16 + (tid >> 4);
+            v[i] = Raw8<T>{};
+            if (row < rows && col < cols) v[i] = load_raw8<T, ALIGNED>(x + row * stride + col);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = (i0 + i) * 16 + (tid >> 4);
+            const int64_t row = band * kTile + r;
+            const bool in = row < rows && col < cols;   // the four lanes of a block agree: cols is a multiple of 32
+            uint32_t byte;
+            const uint32_t w = mx_quantise_quad<T>(v[i], byte);
+            if (in) *reinterpret_cast<uint32_t *>(codes + row * (cols / 2) + col / 2) = w;
+            if ((sub & 3) == 0) tile[mx_scale_at(r, sub >> 2)] = (uint8_t)(in ? byte : 0u);   // padding: 2^-127, which times a zero code is nothing
+        }
     }
     __syncthreads();
     if (tid < 32) reinterpret_cast<uint4 *>(scales + (size_t)blockIdx.x * 512)[tid] = reinterpret_cast<const uint4 *>(tile)[tid];

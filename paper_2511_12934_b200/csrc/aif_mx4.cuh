@@ -13,11 +13,10 @@ namespace {
 constexpr int kMxBlock = 32;      // elements that share a scale
 constexpr uint32_t kMxNan = 255;  // scale byte of a block that holds an infinity or NaN: every value of it is NaN
 
-// Scale byte of a block whose largest magnitude has these bits (fp32, sign off): the exponent of the largest value less the two of
+// Scale byte of a block whose largest magnitude has this exponent field: the exponent of the largest value less the two of
 // the largest code, never below 2^-127.  A plain difference of exponent fields, subnormal blocks included.
-__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t top_bits)
+__device__ __forceinline__ uint32_t mx_scale_byte(uint32_t field)
 {
-    const uint32_t field = top_bits >> 23;
     return field == 255u ? kMxNan : field > 2u ? field - 2u : 0u;
 }
 // 2^(127 - byte) for the byte of a block without infinities; its products with the block's elements are exact.
@@ -60,22 +59,48 @@ __device__ __forceinline__ void mx_decode8_f16(uint32_t w, uint32_t (&o)[4])
 }
 __device__ __forceinline__ float2 half2_to_float2(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2 *>(&h)); }
 
-// Eight consecutive elements of storage type T as fp32.  ALIGNED: the address is a multiple of 16 bytes.
+// Eight consecutive elements of storage type T as they are stored.  ALIGNED: the address is a multiple of 16 bytes.
+template <typename T>
+struct Raw8 {
+    uint32_t w[2 * sizeof(T)];
+};
+template <typename T, bool ALIGNED>
+__device__ __forceinline__ Raw8<T> load_raw8(const T *p)
+{
+    Raw8<T> r;
+    if constexpr (!ALIGNED) {
+        if constexpr (sizeof(T) == 2) {
+            const uint16_t *q = reinterpret_cast<const uint16_t *>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r.w[i] = (uint32_t)__ldg(q + 2 * i) | (uint32_t)__ldg(q + 2 * i + 1) << 16;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r.w[i] = __float_as_uint(__ldg(p + i));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const uint4 x = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+            r.w[4 * i] = x.x, r.w[4 * i + 1] = x.y, r.w[4 * i + 2] = x.z, r.w[4 * i + 3] = x.w;
+        }
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw8<T> &r, float (&v)[8])
+{
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(r.w[i] << 16), v[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r.w[i]);
+    }
+}
 template <typename T, bool ALIGNED>
 __device__ __forceinline__ void load8(const T *p, float (&v)[8])
 {
-    if constexpr (!ALIGNED) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)p[i];
-    } else if constexpr (sizeof(T) == 2) {
-        const uint4 r = __ldg(reinterpret_cast<const uint4 *>(p));
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    } else {
-        const float4 a = __ldg(reinterpret_cast<const float4 *>(p)), b = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    }
+    widen8<T>(load_raw8<T, ALIGNED>(p), v);
 }
 template <typename T, bool ALIGNED>
 __device__ __forceinline__ void store8(T *p, const float (&v)[8])
@@ -97,20 +122,39 @@ __device__ __forceinline__ void store8(T *p, const float (&v)[8])
     }
 }
 
-// Four neighbouring lanes (4 i .. 4 i + 3, converged) quantise the 32 elements of one block, eight each: the lane's codes, and the block's scale byte.
-__device__ __forceinline__ uint32_t mx_quantise_quad(const float (&x)[8], uint32_t &byte)
+// Larger of two pairs of bf16 magnitudes; NaN is the largest.
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b)
 {
-    uint32_t top = 0;
+    uint32_t o;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
+    return o;
+}
+// Four neighbouring lanes (4 i .. 4 i + 3, converged) quantise the 32 elements of one block, eight each: the lane's codes, and the block's scale byte.
+template <typename T>
+__device__ __forceinline__ uint32_t mx_quantise_quad(const Raw8<T> &x, uint32_t &byte)
+{
+    uint32_t field;   // exponent field of the largest magnitude
+    if constexpr (sizeof(T) == 2) {
+        uint32_t m = max_bf16x2(max_bf16x2(x.w[0] & 0x7fff7fffu, x.w[1] & 0x7fff7fffu), max_bf16x2(x.w[2] & 0x7fff7fffu, x.w[3] & 0x7fff7fffu));
+        m = max_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        field = max((m & 0xffffu) >> 7, m >> 23);
+    } else {
+        uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);   // as integers: NaN stays the largest
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    byte = mx_scale_byte(top);
+        for (int i = 0; i < 8; ++i) top = max(top, x.w[i] & 0x7fffffffu);   // as integers: NaN stays the largest
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        field = top >> 23;
+    }
+    byte = mx_scale_byte(field);
     const float inv = mx_inverse_scale(byte);
-    float y[8];
+    float v[8];
+    widen8<T>(x, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = byte == kMxNan ? 0.f : x[i] * inv;
-    return mx_encode8(y);
+    for (int i = 0; i < 8; ++i) v[i] *= inv;
+    const uint32_t w = mx_encode8(v);
+    return byte == kMxNan ? 0u : w;
 }
 // The values of eight codes of a block with this scale.
 __device__ __forceinline__ void mx_values8(uint32_t codes, float scale, float (&v)[8])
