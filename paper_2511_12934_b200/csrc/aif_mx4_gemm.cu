@@ -75,7 +75,7 @@ struct GemmParams {
     int32_t relu;
     void *out;
     int64_t out_stride;
-    int32_t wide;        // rows of `out` begin on 16-byte boundaries
+    int32_t wide;        // rows of `out` begin and end on 16-byte boundaries: tile stores
     int32_t n_tiles;     // column tiles
     int64_t tiles;
     uint32_t *status;
@@ -349,7 +349,8 @@ int aif_mx4_linear(const aif_mx4_product *q, aif_stream stream)
     GemmParams p{};
     p.m = q->m, p.n = q->n, p.k = q->k, p.a_scales = scales, p.w_scales = q->w_scales, p.bias = q->bias, p.relu = q->relu;
     p.out = q->out, p.out_stride = q->out_stride, p.status = q->status;
-    p.wide = (reinterpret_cast<uintptr_t>(q->out) & 15) == 0 && (q->out_stride * el) % 16 == 0;
+    // (a tile store cuts a row off at 16 bytes, not at an element)
+    p.wide = (reinterpret_cast<uintptr_t>(q->out) & 15) == 0 && (q->out_stride * el) % 16 == 0 && ((int64_t)q->n * el) % 16 == 0;
     if (e == cudaSuccess) e = q->dtype == AIF_BF16 ? run_gemm<__nv_bfloat16>(p, codes, q->w_codes, st) : run_gemm<float>(p, codes, q->w_codes, st);
     if (e == cudaSuccess) return AIF_OK;
     char text[256];
