@@ -476,7 +476,7 @@ typedef struct {
     float scale;               /* > 0, or 0: 1 / sqrt(d) */
     int32_t window, sinks;     /* window 0: all rows are visible, sinks is not used */
     int32_t pad_;
-    void *workspace;           /* aif_cache4_attention_workspace bytes, 16-byte aligned; not shared with a call that may run at the same time */
+    void *workspace;           /* aif_cache4_attention_workspace bytes (0: not used), 16-byte aligned; not shared with a call that may run at the same time */
     int64_t workspace_bytes;
 } aif_cache4_query;
 int64_t aif_cache4_attention_workspace(const aif_cache4 *c, const aif_cache4_query *q);

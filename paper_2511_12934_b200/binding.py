@@ -444,14 +444,18 @@ class Aif:
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 class _Launch:
     """The device of a call's tensors made current, and the raw stream; `alloc` allocates for use on that stream."""
+    __slots__ = ("device", "stream", "other", "raw")
 
     def __init__(self, device: torch.device, stream):
         if stream is not None and stream.device != device:
             raise ValueError(f"stream on {stream.device}, tensors on {device}")
         self.device, self.stream = device, stream
-        self.other = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+        self.other = torch.cuda.device(device) if _current_device() != device.index else None
 
     def __enter__(self):
         if self.other is not None:
@@ -470,15 +474,16 @@ class _Launch:
             return torch.empty(n, dtype=torch.uint8, device=self.device)
 
 
-def _tensor(t, name: str, dtype, shape, device: torch.device, dense: bool = True) -> torch.Tensor:
-    """`t` checked: on `device`, of dtype and shape (None: any size), contiguous (dense) or at least with its rows in one piece."""
+def _tensor(t, name: str, dtype, shape, device: torch.device) -> torch.Tensor:
+    """`t` checked: contiguous, on `device`, of dtype and shape (None: any size)."""
     if not isinstance(t, torch.Tensor) or t.device != device:
         raise ValueError(f"{name}: a tensor on {device} is needed")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name}: {dtype} is needed, not {t.dtype}")
-    if t.dim() != len(shape) or any(w is not None and w != g for w, g in zip(shape, t.shape)):
-        raise ValueError(f"{name}: shape {tuple(shape)} is needed, not {tuple(t.shape)}")
-    if dense and not t.is_contiguous():
+    got = t.shape
+    if len(got) != len(shape) or (got != shape and any(w is not None and w != g for w, g in zip(shape, got))):
+        raise ValueError(f"{name}: shape {tuple(shape)} is needed, not {tuple(got)}")
+    if not t.is_contiguous():
         raise ValueError(f"{name}: not contiguous")
     return t
 
@@ -487,13 +492,14 @@ def _rows(t: torch.Tensor, name: str, heads: int, d: int, device: torch.device, 
     """[rows x heads x d] (or [rows x d] with one head), fp32 or bf16, a row in one piece: the elements from row to row."""
     if not isinstance(t, torch.Tensor) or t.device != device:
         raise ValueError(f"{name}: a tensor on {device} is needed")
-    if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
+    if t.dtype not in _DTYPES or (dtype is not None and t.dtype is not dtype):
         raise ValueError(f"{name}: {dtype or 'float32 or bfloat16'} is needed, not {t.dtype}")
-    if tuple(t.shape[1:]) != (heads, d) and not (heads == 1 and tuple(t.shape[1:]) == (d,)):
-        raise ValueError(f"{name}: shape [rows, {heads}, {d}] is needed, not {tuple(t.shape)}")
-    if t.stride(-1) != 1 or (t.dim() == 3 and heads > 1 and t.stride(1) != d):
+    got, step = t.shape, t.stride()
+    if not (len(got) == 3 and got[1] == heads and got[2] == d) and not (heads == 1 and len(got) == 2 and got[1] == d):
+        raise ValueError(f"{name}: shape [rows, {heads}, {d}] is needed, not {tuple(got)}")
+    if step[-1] != 1 or (heads > 1 and step[1] != d):
         raise ValueError(f"{name}: the heads of a row have to lie one after the other")
-    return t.stride(0) if t.shape[0] > 1 else heads * d
+    return step[0] if got[0] > 1 else heads * d
 
 
 def _cuda_device(t, name: str) -> torch.device:
@@ -517,11 +523,11 @@ class Mx4(NamedTuple):
 
 
 def _mx4_check(m: Mx4, name: str, device: torch.device) -> Mx4:
-    _tensor(m.codes, name + ".codes", torch.uint8, (None, None), device)
-    n = load_library().aif_mx4_scale_bytes(m.rows, m.cols)
+    codes = _tensor(m.codes, name, torch.uint8, (None, None), device)
+    n = load_library().aif_mx4_scale_bytes(codes.shape[0], 2 * codes.shape[1])
     if n < 0:
         _check(n, name)
-    _tensor(m.scales, name + ".scales", torch.uint8, (n,), device)
+    _tensor(m.scales, name, torch.uint8, (n,), device)
     return m
 
 
@@ -569,32 +575,32 @@ def mx4_linear(x, w: Mx4, out: torch.Tensor, bias: Optional[torch.Tensor] = None
     status: a uint32-sized int32 tensor that takes AIF_STATUS_TIMEOUT."""
     device = _cuda_device(out, "out")
     _mx4_check(w, "w", device)
-    m, n, k = out.shape[0], w.rows, w.cols
-    p = aif_mx4_product()
-    p.struct_size, p.m, p.n, p.k, p.relu = C.sizeof(aif_mx4_product), m, n, k, 1 if relu else 0
-    p.out_stride = _rows(out, "out", 1, n, device)
-    p.dtype, p.out = _DTYPES[out.dtype], out.data_ptr()
-    p.w_codes, p.w_scales = w.codes.data_ptr(), w.scales.data_ptr()
+    (n, k), m = w.codes.shape, out.shape[0]
+    k *= 2
+    out_stride = _rows(out, "out", 1, n, device)
     if bias is not None:
-        p.bias = _tensor(bias, "bias", torch.float32, (n,), device).data_ptr()
+        _tensor(bias, "bias", torch.float32, (n,), device)
     if status is not None:
-        p.status = _tensor(status, "status", torch.int32, (1,), device).data_ptr()
-    rows = x.rows if isinstance(x, Mx4) else x.shape[0]
-    if rows != m:
-        raise ValueError(f"x: {m} rows are needed, not {rows}")
+        _tensor(status, "status", torch.int32, (1,), device)
+    quantised = isinstance(x, Mx4)
+    if (x.rows if quantised else x.shape[0]) != m:
+        raise ValueError(f"x: {m} rows are needed, not {x.rows if quantised else x.shape[0]}")
+    if quantised:
+        if x.cols != k:
+            raise ValueError(f"x: {k} columns are needed, not {x.cols}")
+        _mx4_check(x, "x", device)
+        x_args = (None, 0, x.codes.data_ptr(), x.scales.data_ptr())
+    else:
+        x_args = (x.data_ptr(), _rows(x, "x", 1, k, device, out.dtype), None, None)
+    p = aif_mx4_product(C.sizeof(aif_mx4_product), _DTYPES[out.dtype], m, n, k, *x_args, w.codes.data_ptr(), w.scales.data_ptr(),
+                        None if bias is None else bias.data_ptr(), out.data_ptr(), out_stride, None, 0, None if status is None else status.data_ptr(), 1 if relu else 0)
+    lib = load_library()
     with _Launch(device, stream) as at:
-        keep = None
-        if isinstance(x, Mx4):
-            if x.cols != k:
-                raise ValueError(f"x: {k} columns are needed, not {x.cols}")
-            _mx4_check(x, "x", device)
-            p.x_codes, p.x_scales = x.codes.data_ptr(), x.scales.data_ptr()
-        else:
-            p.x_stride = _rows(x, "x", 1, k, device, out.dtype)
-            p.x = x.data_ptr()
-            keep = at.alloc(max(16, load_library().aif_mx4_workspace_bytes(m, k)))
+        if not quantised:
+            n_bytes = lib.aif_mx4_workspace_bytes(m, k)
+            keep = at.alloc(max(16, n_bytes))
             p.workspace, p.workspace_bytes = keep.data_ptr(), keep.numel()
-        _check(load_library().aif_mx4_linear(C.byref(p), at.raw), "aif_mx4_linear")
+        _check(lib.aif_mx4_linear(C.byref(p), at.raw), "aif_mx4_linear")
     return out
 
 
@@ -632,7 +638,7 @@ class Cache4:
             t = getattr(self, name)
             setattr(c, name, None if t is None else t.data_ptr())
         c.scratch = self._scratch.data_ptr()
-        self._c = c
+        self._c, self._ref = c, C.byref(c)
         self.reset(stream=stream)
 
     def _ids(self, t: torch.Tensor, name: str) -> int:
@@ -651,14 +657,14 @@ class Cache4:
     def reset(self, stream=None):
         """Empties the cache."""
         with _Launch(self.device, stream) as at:
-            _check(self.lib.aif_cache4_reset(C.byref(self._c), at.raw), "aif_cache4_reset")
+            _check(self.lib.aif_cache4_reset(self._ref, at.raw), "aif_cache4_reset")
 
     def append(self, seq_ids: torch.Tensor, offsets: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor] = None, stream=None):
         """Rows offsets[i] .. offsets[i + 1] of k (and v) to the end of sequence seq_ids[i]."""
         n = self._ids(seq_ids, "seq_ids")
         stride = self._rows(offsets, n, k, v, "k", "v")
         with _Launch(self.device, stream) as at:
-            _check(self.lib.aif_cache4_append(C.byref(self._c), n, seq_ids.data_ptr(), offsets.data_ptr(), k.data_ptr(), None if v is None else v.data_ptr(),
+            _check(self.lib.aif_cache4_append(self._ref, n, seq_ids.data_ptr(), offsets.data_ptr(), k.data_ptr(), None if v is None else v.data_ptr(),
                                               _DTYPES[k.dtype], k.shape[0], stride, at.raw), "aif_cache4_append")
 
     def read(self, seq_ids: torch.Tensor, offsets: torch.Tensor, k_out: torch.Tensor, v_out: Optional[torch.Tensor] = None, stream=None):
@@ -666,14 +672,14 @@ class Cache4:
         n = self._ids(seq_ids, "seq_ids")
         stride = self._rows(offsets, n, k_out, v_out, "k_out", "v_out")
         with _Launch(self.device, stream) as at:
-            _check(self.lib.aif_cache4_read(C.byref(self._c), n, seq_ids.data_ptr(), offsets.data_ptr(), k_out.data_ptr(),
+            _check(self.lib.aif_cache4_read(self._ref, n, seq_ids.data_ptr(), offsets.data_ptr(), k_out.data_ptr(),
                                             None if v_out is None else v_out.data_ptr(), _DTYPES[k_out.dtype], k_out.shape[0], stride, at.raw), "aif_cache4_read")
 
     def _share(self, call, src: torch.Tensor, dst: torch.Tensor, stream):
         n = self._ids(src, "src")
         _tensor(dst, "dst", torch.int32, (n,), self.device)
         with _Launch(self.device, stream) as at:
-            _check(call(C.byref(self._c), n, src.data_ptr(), dst.data_ptr(), at.raw), call.__name__)
+            _check(call(self._ref, n, src.data_ptr(), dst.data_ptr(), at.raw), call.__name__)
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor, stream=None):
         """Sequence dst[i] becomes a snapshot of src[i] on the same pages."""
@@ -686,14 +692,14 @@ class Cache4:
     def free(self, seq_ids: torch.Tensor, stream=None):
         n = self._ids(seq_ids, "seq_ids")
         with _Launch(self.device, stream) as at:
-            _check(self.lib.aif_cache4_free(C.byref(self._c), n, seq_ids.data_ptr(), at.raw), "aif_cache4_free")
+            _check(self.lib.aif_cache4_free(self._ref, n, seq_ids.data_ptr(), at.raw), "aif_cache4_free")
 
     def compact(self, into: "Cache4", stream=None):
         """All sequences into the cache `into`, pages in use first and in their order."""
         if into.device != self.device:
             raise ValueError(f"into: a cache on {self.device} is needed")
         with _Launch(self.device, stream) as at:
-            _check(self.lib.aif_cache4_compact(C.byref(self._c), C.byref(into._c), at.raw), "aif_cache4_compact")
+            _check(self.lib.aif_cache4_compact(self._ref, into._ref, at.raw), "aif_cache4_compact")
 
     def attention(self, q: torch.Tensor, out: torch.Tensor, seq_ids: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None, scale: float = 0.0,
                   window: int = 0, sinks: int = 0, stream=None) -> torch.Tensor:
@@ -702,34 +708,29 @@ class Cache4:
         heads = q.shape[1] if q.dim() == 3 else 1
         if heads < 1 or heads % self.heads:
             raise ValueError(f"q: a multiple of {self.heads} heads is needed, not {heads}")
-        a = aif_cache4_query()
-        a.struct_size, a.n_heads, a.rows = C.sizeof(aif_cache4_query), heads, q.shape[0]
-        a.q_stride = _rows(q, "q", heads, self.d, self.device)
-        a.dtype, a.q = _DTYPES[q.dtype], q.data_ptr()
-        a.out_stride = _rows(out, "out", heads, self.d, self.device, q.dtype)
-        if out.shape[0] != q.shape[0]:
-            raise ValueError(f"out: {q.shape[0]} rows are needed, not {out.shape[0]}")
-        a.out = out.data_ptr()
-        a.n = q.shape[0]
-        if seq_ids is not None:
-            a.n, a.seq_ids = self._ids(seq_ids, "seq_ids"), seq_ids.data_ptr()
-        elif offsets is not None:
-            a.n = max(0, offsets.numel() - 1)
+        rows, device = q.shape[0], self.device
+        q_stride, out_stride = _rows(q, "q", heads, self.d, device), _rows(out, "out", heads, self.d, device, q.dtype)
+        if out.shape[0] != rows:
+            raise ValueError(f"out: {rows} rows are needed, not {out.shape[0]}")
+        n = rows if seq_ids is None and offsets is None else self._ids(seq_ids, "seq_ids") if seq_ids is not None else max(0, offsets.numel() - 1)
         if offsets is not None:
-            a.offsets = _tensor(offsets, "offsets", torch.int64, (a.n + 1,), self.device).data_ptr()
-        a.scale, a.window, a.sinks = scale, window, sinks
-        n_bytes = self.lib.aif_cache4_attention_workspace(C.byref(self._c), C.byref(a))
+            _tensor(offsets, "offsets", torch.int64, (n + 1,), device)
+        a = aif_cache4_query(C.sizeof(aif_cache4_query), _DTYPES[q.dtype], heads, n, None if seq_ids is None else seq_ids.data_ptr(),
+                             None if offsets is None else offsets.data_ptr(), rows, q.data_ptr(), out.data_ptr(), q_stride, out_stride, scale, window, sinks)
+        ref = C.byref(a)
+        n_bytes = self.lib.aif_cache4_attention_workspace(self._ref, ref)
         if n_bytes < 0:
             _check(n_bytes, "aif_cache4_attention")
-        with _Launch(self.device, stream) as at:
-            keep = at.alloc(max(16, n_bytes))
-            a.workspace, a.workspace_bytes = keep.data_ptr(), keep.numel()
-            _check(self.lib.aif_cache4_attention(C.byref(self._c), C.byref(a), at.raw), "aif_cache4_attention")
+        with _Launch(device, stream) as at:
+            if n_bytes:
+                keep = at.alloc(n_bytes)
+                a.workspace, a.workspace_bytes = keep.data_ptr(), n_bytes
+            _check(self.lib.aif_cache4_attention(self._ref, ref, at.raw), "aif_cache4_attention")
         return out
 
     def poll_status(self, stream=None) -> int:
         """Status bits since the last call (STATUS_BAD_ID, STATUS_FULL, STATUS_TIMEOUT); waits for the stream."""
         bits = C.c_uint32()
         with _Launch(self.device, stream) as at:
-            _check(self.lib.aif_cache4_poll(C.byref(self._c), C.byref(bits), at.raw), "aif_cache4_poll")
+            _check(self.lib.aif_cache4_poll(self._ref, C.byref(bits), at.raw), "aif_cache4_poll")
         return int(bits.value)

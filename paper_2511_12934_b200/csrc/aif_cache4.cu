@@ -1,7 +1,7 @@
 // Books and rows of the 4-bit sequence cache: appending, sharing, copying, moving, freeing and reading pages.
 //
 // A call that changes the books is one small kernel over the listed sequences (k_books) and, where rows or pages move, one more that
-// moves them, bound by HBM.  The books are kept by one cluster of CTAs (a single CTA for a few sequences): its phases hand over through cluster
+// moves them, bound by HBM.  The books are kept by one CTA, or for many pages one cluster of CTAs: its phases hand over through
 // barriers, a matter of a microsecond, where separate launches would cost two or three each.  Nothing depends on the order of atomics: pages are
 // handed out and taken back by position in the call (prefix sums), so the same calls leave the same books.
 #include <cstdio>
@@ -295,6 +295,212 @@ __global__ void __launch_bounds__(kBookThreads) k_books(const BooksParams p)
             }
         }
     }
+    if (bits) atomicOr(c.status, bits);
+}
+
+// The same for a few sequences (n <= kFewSeqs), in one CTA with the entries in shared memory.  Its time is a chain of loads from L2, so none is made twice.
+constexpr int kFewSeqs = 128, kFewThreads = 1024;
+
+// before[i] = count[0] + .. + count[i - 1]; the total is left in before[n].  One warp.
+__device__ __forceinline__ void scan_few(const int32_t *count, int32_t *before, int n, int lane)
+{
+    int v[4], mine = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = 4 * lane + u < n ? count[4 * lane + u] : 0, mine += v[u];
+    int x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    int at = x - mine;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if (4 * lane + u <= n) before[4 * lane + u] = at;
+        at += v[u];
+    }
+    if (lane == 31 && n == kFewSeqs) before[n] = at;
+}
+
+template <int OP>
+__global__ void __launch_bounds__(kFewThreads) k_books_few(const BooksParams p)
+{
+    const Cache4 &c = p.c;
+    const Scratch s = scratch_of(c);
+    __shared__ int32_t dst[kFewSeqs], src[kFewSeqs], had[kFewSeqs], now[kFewSeqs], count[kFewSeqs], before[kFewSeqs + 1], info[kFewSeqs], from[kFewSeqs], to[kFewSeqs];
+    __shared__ int32_t n_free, given;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n;
+    constexpr int kWarps = kFewThreads / 32;
+    uint32_t bits = 0;
+    bool offsets_bad = false;
+    int64_t added = 0;
+    if (tid == 0) n_free = min(max(ld(c.n_free), 0), c.n_pages), given = 0;
+    if (tid < n) {
+        const int q = p.dst[tid], f = OP == kFork || OP == kCopy ? p.src[tid] : 0;
+        dst[tid] = q, src[tid] = f;
+        if (OP == kAppend) {
+            const int64_t a = p.offsets[tid], b = p.offsets[tid + 1];
+            offsets_bad = a < 0 || b < a || b > p.rows;
+            added = b - a;
+        }
+        had[tid] = q >= 0 && q < c.n_seqs ? ld(c.lengths + q) : 0;
+        now[tid] = (OP == kFork || OP == kCopy) && f >= 0 && f < c.n_seqs ? ld(c.lengths + f) : 0;
+    }
+    offsets_bad = __syncthreads_or(offsets_bad) != 0;
+    if (tid < n) {
+        const int q = dst[tid], f = src[tid];
+        bool ok = q >= 0 && q < c.n_seqs;
+        for (int j = 0; j < tid; ++j) ok = ok && dst[j] != q;   // the first that names a sequence stands
+        if (OP == kFork || OP == kCopy) {
+            ok = ok && f >= 0 && f < c.n_seqs;
+            for (int j = 0; j < n; ++j) ok = ok && dst[j] != f;
+        }
+        if (!ok || offsets_bad) bits |= AIF_STATUS_BAD_ID;
+        int need = 0, tail = -1, in = ok && !offsets_bad ? 0 : -1;
+        if (OP == kAppend && in == 0) {
+            const int L = had[tid];
+            if (L < 0 || L > c.longest() || added > c.longest() - L) {
+                in = -1, bits |= AIF_STATUS_FULL;
+            } else {
+                in = L;
+                need = c.pages_of(L + (int)added) - c.pages_of(L);
+                now[tid] = L + (int)added;
+                if (added > 0 && (L & (c.page_rows() - 1)) > 0) {
+                    const int pg = ld(c.table + (size_t)q * c.max_pages + (L >> c.page_shift));
+                    if (c.holds(pg) && ld(c.refs + pg) > 1) tail = pg, need += 1;
+                }
+            }
+        }
+        if (OP == kCopy && in == 0) need = min(c.pages_of(max(now[tid], 0)), c.max_pages);
+        info[tid] = in, from[tid] = tail, to[tid] = -1, count[tid] = need;
+    }
+    __syncthreads();
+    auto pages_had = [&](int i) { return min(c.pages_of(max(had[i], 0)), c.max_pages); };
+    if (OP != kAppend) {
+        // the pages that the entries' sequences had: one reference less each, then those that nobody has back to the free ones
+        __shared__ int32_t back[kFewSeqs];
+        for (int i = warp; i < n; i += kWarps) {
+            if (info[i] < 0) continue;
+            const int32_t *row = c.table + (size_t)dst[i] * c.max_pages;
+            const int np = pages_had(i);
+            for (int x = lane; x < np; x += 32) {
+                const int pg = ld(row + x);
+                if (c.holds(pg)) atomicSub(c.refs + pg, 1), atomicMin(s.mark_page + pg, i * c.max_pages + x);
+            }
+        }
+        __syncthreads();
+        for (int i = warp; i < n; i += kWarps) {
+            int got = 0;
+            if (info[i] >= 0) {
+                const int32_t *row = c.table + (size_t)dst[i] * c.max_pages;
+                const int np = pages_had(i);
+                for (int x = lane; x < np; x += 32) {
+                    const int pg = ld(row + x);
+                    if (!c.holds(pg)) continue;
+                    const int refs = ld(c.refs + pg), mark = ld(s.mark_page + pg);
+                    got += refs == 0 && mark == i * c.max_pages + x;
+                }
+                got = __reduce_add_sync(0xffffffffu, got);
+            }
+            if (lane == 0) back[i] = got;
+        }
+        __syncthreads();
+        if (warp == 0) scan_few(back, before, n, lane);
+        __syncthreads();
+        const int total = before[n], base = n_free;
+        for (int i = warp; i < n; i += kWarps) {
+            if (info[i] < 0) continue;
+            int32_t *row = c.table + (size_t)dst[i] * c.max_pages;
+            const int np = pages_had(i), nf = OP == kFork ? min(c.pages_of(max(now[i], 0)), c.max_pages) : 0;
+            const int32_t *row_f = c.table + (size_t)max(src[i], 0) * c.max_pages;
+            // pages go back in the order opposite to the one in which they are handed out: the last entry's last page first
+            int at = base + total - before[i] - 1;
+            for (int x0 = 0; x0 < max(np, nf); x0 += 32) {
+                const int x = x0 + lane, pg = x < np ? ld(row + x) : -1, take = x < nf ? ld(row_f + x) : -1;
+                int refs = 1, mark = -1;
+                if (c.holds(pg)) refs = ld(c.refs + pg), mark = ld(s.mark_page + pg);
+                const bool mine = mark == i * c.max_pages + x && c.holds(pg), give = mine && refs == 0;
+                const unsigned who = __ballot_sync(0xffffffffu, give);
+                const int pos = at - __popc(who & ((1u << lane) - 1u));
+                if (give && pos >= 0 && pos < c.n_pages) st(c.free_pages + pos, pg);
+                if (mine) st(s.mark_page + pg, INT_MAX);
+                if (x < np || x < nf) st(row + x, take);
+                if (c.holds(take)) atomicAdd(c.refs + take, 1);
+                at -= __popc(who);
+            }
+            if (lane == 0) st(c.lengths + dst[i], OP == kFork ? now[i] : 0);
+        }
+        __syncthreads();
+        if (tid == 0) n_free = base + total;
+        __syncthreads();
+    }
+    if (OP == kCopy || OP == kAppend) {
+        if (warp == 0) scan_few(count, before, n, lane);
+        __syncthreads();
+        const int top = n_free - 1;
+        for (int i = warp; i < n; i += kWarps) {
+            const int need = count[i], first = before[i], in = info[i];
+            if (in < 0) continue;
+            if (need > 0 && first + need > top + 1) {   // the entries that are served are a beginning of those that need pages
+                bits |= AIF_STATUS_FULL;
+                __syncwarp();
+                if (lane == 0) info[i] = -1, from[i] = -1;
+                continue;
+            }
+            int32_t *row = c.table + (size_t)dst[i] * c.max_pages;
+            const int tail = from[i], have = OP == kAppend ? c.pages_of(in) - (tail >= 0) : 0;   // place of the first new page
+            for (int x = lane; x < need; x += 32) {
+                const int pg = ld(c.free_pages + top - first - x);
+                if (c.holds(pg)) st(c.refs + pg, 1);
+                else bits |= AIF_STATUS_BAD_ID;
+                st(row + have + x, pg);
+                if (x == 0 && tail >= 0) {
+                    to[i] = pg, given = 1;
+                    atomicSub(c.refs + tail, 1), atomicMin(s.mark_page + tail, i);
+                }
+            }
+            if (lane == 0) {
+                st(c.lengths + dst[i], now[i]);
+                if (OP == kCopy) info[i] = need;
+            }
+        }
+        __syncthreads();
+        if (tid < n) {
+            st(s.info + tid, info[tid]), st(s.from + tid, from[tid]), st(s.to + tid, to[tid]);
+        }
+        // pages taken: up to the last entry that was served
+        int taken = 0;
+        if (tid < n && count[tid] > 0 && before[tid] + count[tid] <= top + 1) taken = before[tid] + count[tid];
+        taken = __reduce_max_sync(0xffffffffu, taken);
+        __shared__ int32_t most;
+        if (tid == 0) most = 0;
+        __syncthreads();
+        if (lane == 0 && taken > 0) atomicMax(&most, taken);
+        __syncthreads();
+        if (tid == 0) n_free -= most;
+        __syncthreads();
+        if (OP == kAppend && given) {
+            // shared last pages that every sequence has copied away in this very call belong to nobody now
+            int pg = -1;
+            bool mine = false;
+            if (tid < n) {
+                pg = from[tid];
+                mine = pg >= 0 && ld(s.mark_page + pg) == tid;
+                count[tid] = mine && ld(c.refs + pg) == 0 ? 1 : 0;
+            }
+            __syncthreads();
+            if (warp == 0) scan_few(count, before, n, lane);
+            __syncthreads();
+            if (tid < n) {
+                const int pos = n_free + before[n] - 1 - before[tid];
+                if (count[tid] && pos >= 0 && pos < c.n_pages) st(c.free_pages + pos, pg);
+                if (mine) st(s.mark_page + pg, INT_MAX);
+            }
+            __syncthreads();
+            if (tid == 0) n_free += before[n];
+        }
+    }
+    if (tid == 0) st(c.n_free, n_free);
     if (bits) atomicOr(c.status, bits);
 }
 
@@ -605,15 +811,18 @@ __global__ void __launch_bounds__(256) k_reset(const Cache4 c)
 template <int OP>
 cudaError_t run_books(const BooksParams &p, cudaStream_t st)
 {
+    count_launch();
+    // A few sequences: one CTA, %%% us against %%% (48 sequences of 32 pages forked), until its 32 warps have some hundred pages each.
+    if (p.n <= kFewSeqs && (int64_t)p.n * p.c.max_pages <= 32768) {
+        k_books_few<OP><<<1, kFewThreads, 0, st>>>(p);
+        return cudaGetLastError();
+    }
     cudaLaunchConfig_t cfg{};
-    // a few sequences: one CTA; its barriers cost less than a cluster's
-    const unsigned ctas = p.n <= 16 ? 1 : 8;
-    cfg.gridDim = dim3(ctas), cfg.blockDim = dim3(kBookThreads), cfg.stream = st;
+    cfg.gridDim = dim3(8), cfg.blockDim = dim3(kBookThreads), cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = ctas, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = 8, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr, cfg.numAttrs = 1;
-    count_launch();
     return cudaLaunchKernelEx(&cfg, k_books<OP>, p);
 }
 

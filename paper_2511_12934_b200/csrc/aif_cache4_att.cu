@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_att4_rows(const AttCall a)
     const int64_t total = plan_total(a, plan);
     const int ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, total / a.min_units));
     const int cta = blockIdx.x;
-    if (tid == 0) a.headers[cta].first_cta = -1;
+    if (tid == 0 && a.headers) a.headers[cta].first_cta = -1;
     if (total == 0 || cta >= ctas) return;
     const int64_t u1 = cut(total, ctas, cta + 1);
     int64_t u = cut(total, ctas, cta);
@@ -341,9 +341,8 @@ template <typename T, int R, int P, bool SHARED>
 cudaError_t run_rows_at(const AttCall &a, int grid, cudaStream_t st)
 {
     const size_t smem = (size_t)kRowWarps * kRing * (SHARED ? 1 : 2) * RowsCfg<R, P>::kKeys * (a.c.d / 2 + a.c.d / 32) + (size_t)kRowWarps * R * (a.c.d + 2) * 4;
-    // (an attribute of the device's copy of the kernel: set for whichever device is current)
     if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(k_att4_rows<T, R, P, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = allow_smem<k_att4_rows<T, R, P, SHARED>>(200 * 1024);
         if (e != cudaSuccess) return e;
     }
     count_launch();
@@ -364,8 +363,9 @@ cudaError_t run_rows(const AttCall &a, int grid, cudaStream_t st)
 struct AttForm {
     enum { kRows, kFew, kPair, kTensor } kernel;
     int tile_rows, block_keys, grid, min_units;
+    bool cut;   // a tile may have several units, and so be cut between CTAs
 };
-AttForm form_of(const aif_cache4 *c, const aif_cache4_query *q)
+AttForm kernel_of(const aif_cache4 *c, const aif_cache4_query *q)
 {
     const int64_t group = q->n_heads / c->heads, per_seq = (q->rows + q->n - 1) / q->n * group;   // query rows of a sequence and a head of the cache, on average
     const bool bf = q->dtype == AIF_BF16;
@@ -374,9 +374,18 @@ AttForm form_of(const aif_cache4 *c, const aif_cache4_query *q)
     if (bf && (c->d == 32 || c->d == 64 || c->d == 128 || c->d == 256)) return {AttForm::kFew, 8, -16, c->d == 256 ? 296 : 444, 1};
     return {AttForm::kRows, per_seq <= 2 ? 1 : 4, -kRowGroups, 444, 1};
 }
+AttForm form_of(const aif_cache4 *c, const aif_cache4_query *q)
+{
+    AttForm f = kernel_of(c, q);
+    // most rows that a sequence can show: what its pages hold, or the window and the first rows (which may begin inside a group of 16)
+    int64_t most = (int64_t)c->max_pages * c->page_rows;
+    if (q->window > 0) most = std::min<int64_t>(most, (int64_t)q->window + q->sinks + 32);
+    f.cut = most > (f.block_keys > 0 ? f.block_keys : -16 * f.block_keys);
+    return f;
+}
 int64_t workspace_of(const AttForm &f, const aif_cache4 *c)
 {
-    return (int64_t)f.grid * (int64_t)sizeof(PieceHeader) + 2ll * f.grid * f.tile_rows * (c->d + 2) * 4;
+    return f.cut ? (int64_t)f.grid * (int64_t)sizeof(PieceHeader) + 2ll * f.grid * f.tile_rows * (c->d + 2) * 4 : 0;
 }
 
 int check_query(const aif_cache4 *c, const aif_cache4_query *q)
@@ -418,15 +427,14 @@ int aif_cache4_attention(const aif_cache4 *c, const aif_cache4_query *q, aif_str
     if (q->n == 0 || q->rows == 0) return AIF_OK;
     if (!q->q || !q->out || !at16(q->q) || !at16(q->out)) return AIF_ERR_ARG;
     const AttForm f = form_of(c, q);
-    if (!q->workspace || !at16(q->workspace) || q->workspace_bytes < workspace_of(f, c)) return AIF_ERR_ARG;
+    if (f.cut && (!q->workspace || !at16(q->workspace) || q->workspace_bytes < workspace_of(f, c))) return AIF_ERR_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     AttCall a{};
     a.c = cache4_of(c), a.n = q->n, a.n_heads = q->n_heads, a.group = q->n_heads / c->heads, a.seq_ids = q->seq_ids, a.offsets = q->offsets;
     a.rows = q->rows, a.q = q->q, a.out = q->out, a.q_stride = q->q_stride, a.out_stride = q->out_stride;
     a.scale_log2 = 1.4426950408889634f * (q->scale == 0.f ? 1.0f / sqrtf((float)c->d) : q->scale);
     a.window = q->window, a.sinks = q->sinks, a.tile_rows = f.tile_rows, a.block_keys = f.block_keys, a.min_units = f.min_units;
-    a.headers = static_cast<PieceHeader *>(q->workspace);
-    a.records = reinterpret_cast<float *>(a.headers + f.grid);
+    if (f.cut) a.headers = static_cast<PieceHeader *>(q->workspace), a.records = reinterpret_cast<float *>(a.headers + f.grid);
     const bool bf = q->dtype == AIF_BF16, shared = c->shared != 0;
     cudaError_t e;
     if (f.kernel == AttForm::kPair) e = launch_att4_pair(a, f.grid, st);
@@ -438,7 +446,7 @@ int aif_cache4_attention(const aif_cache4 *c, const aif_cache4_query *q, aif_str
     else
         e = bf ? (shared ? run_rows<__nv_bfloat16, 4, true>(a, f.grid, st) : run_rows<__nv_bfloat16, 4, false>(a, f.grid, st))
                : (shared ? run_rows<float, 4, true>(a, f.grid, st) : run_rows<float, 4, false>(a, f.grid, st));
-    if (e == cudaSuccess) {
+    if (e == cudaSuccess && f.cut) {
         const bool tensor = f.kernel == AttForm::kPair || f.kernel == AttForm::kTensor;
         const dim3 grid(f.grid, (f.tile_rows + 7) / 8);
         e = bf ? launch_pdl(k_att4_join<__nv_bfloat16>, grid, dim3(256), 0, st, a, tensor ? 1 : 0) : launch_pdl(k_att4_join<float>, grid, dim3(256), 0, st, a, 0);

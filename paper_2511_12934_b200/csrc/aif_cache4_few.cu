@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(kFewThreads, NB == 8 ? 2 : 3) k_att4_few(const
     const int64_t total = plan_total(a, plan);
     const int ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, total / a.min_units));
     const int cta = blockIdx.x;
-    if (tid == 0) a.headers[cta].first_cta = -1;
+    if (tid == 0 && a.headers) a.headers[cta].first_cta = -1;
     if (total == 0 || cta >= ctas) return;
     const int64_t u1 = cut(total, ctas, cta + 1);
     int64_t u = cut(total, ctas, cta);
@@ -337,7 +337,7 @@ cudaError_t run_few(const AttCall &a, int grid, cudaStream_t st)
 {
     const size_t smem = (size_t)kFewWarps * kFewRows * (32 * NB + 2) * 4;   // up to 65 KB
     if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(k_att4_few<NB, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = allow_smem<k_att4_few<NB, SHARED>>(smem);
         if (e != cudaSuccess) return e;
     }
     count_launch();

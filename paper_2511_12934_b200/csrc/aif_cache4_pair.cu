@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
 
     const int64_t total = plan_total(a, plan);
     const int ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, total / a.min_units)), cta = blockIdx.x;
-    if (tid == 0) a.headers[cta].first_cta = -1;
+    if (tid == 0 && a.headers) a.headers[cta].first_cta = -1;
     const bool work = total > 0 && cta < ctas;
     const int64_t u0 = work ? cut(total, ctas, cta) : 0, u1 = work ? cut(total, ctas, cta + 1) : 0;
     Cursor cur{};
@@ -474,8 +474,7 @@ template <int D, bool SHARED>
 cudaError_t run_pair(const AttCall &a, int grid, cudaStream_t st)
 {
     using C = PairCfg<D, SHARED>;
-    // (an attribute of the device's copy of the kernel: set for whichever device is current)
-    cudaError_t e = cudaFuncSetAttribute(k_att4_pair<D, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+    cudaError_t e = allow_smem<k_att4_pair<D, SHARED>>(C::kSmem);
     if (e != cudaSuccess) return e;
     count_launch();
     return launch_pdl(k_att4_pair<D, SHARED>, dim3(grid), dim3(C::kThreads), C::kSmem, st, a);

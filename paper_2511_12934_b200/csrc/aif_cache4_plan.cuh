@@ -26,7 +26,7 @@ struct AttCall {
     int32_t window, sinks;
     int32_t tile_rows, block_keys, min_units;
     float *records;                // [2 x grid][tile_rows][d] sums, then [tile_rows][2]: exponent offset and weight
-    PieceHeader *headers;   // [grid]
+    PieceHeader *headers;          // [grid]; nullptr where no tile can have more than one unit
 };
 
 // A sequence of the call.

@@ -240,6 +240,20 @@ namespace aif {
 extern std::atomic<uint64_t> g_launches;
 inline void count_launch(int n = 1) { g_launches.fetch_add((uint64_t)n, std::memory_order_relaxed); }
 
+// Lets a kernel have `smem` bytes of dynamic shared memory, once per device and kernel (`Kernel` names it): a driver call less per launch.
+template <auto Kernel>
+inline cudaError_t allow_smem(size_t smem)
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || dev < 0 || dev > 63) return e != cudaSuccess ? e : cudaErrorInvalidDevice;
+    if (done.load(std::memory_order_relaxed) >> dev & 1u) return cudaSuccess;
+    e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+    return e;
+}
+
 // A named host-side range (NVTX) around the launches of a stage or of an entry point: a timeline tool shows the kernels under
 // the stage's name.  With no tool attached a range costs two calls through an empty hook.
 struct StageRange {

@@ -298,8 +298,7 @@ cudaError_t run_gemm(GemmParams p, const uint8_t *a_codes, const uint8_t *w_code
                                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
         if (r != CUDA_SUCCESS) e = cudaErrorInvalidValue;
     }
-    // (an attribute of the device's copy of the kernel: set for whichever device is current)
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_mx4_gemm<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+    if (e == cudaSuccess) e = allow_smem<k_mx4_gemm<T>>(C::kSmem);
     if (e != cudaSuccess) return e;
     p.n_tiles = (p.n + kBN - 1) / kBN;
     p.tiles = (p.m + kBM - 1) / kBM * p.n_tiles;

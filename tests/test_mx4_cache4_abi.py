@@ -72,7 +72,7 @@ def test_product_refusals(lib, change, code):
 def cache(**kw):
     c = B.aif_cache4()
     c.struct_size = C.sizeof(c)
-    base = dict(d=64, heads=2, shared=1, page_rows=32, n_pages=10, n_seqs=4, max_pages=5, k_codes=P, k_scales=P, table=P, lengths=P, refs=P, free_pages=P,
+    base = dict(d=64, heads=2, shared=1, page_rows=32, n_pages=100, n_seqs=4, max_pages=50, k_codes=P, k_scales=P, table=P, lengths=P, refs=P, free_pages=P,
                 n_free=P, scratch=P, status=P)
     for name, value in {**base, **kw}.items():
         setattr(c, name, value)
@@ -143,7 +143,7 @@ def test_row_and_list_refusals(lib):
     other.d = 32
     assert lib.aif_cache4_compact(c, C.byref(other), None) == B.ERR_SHAPE
     assert lib.aif_cache4_compact(c, c, None) == B.ERR_ARG
-    assert lib.aif_cache4_scratch_ints(c) > 2 * 10 + 6 * 4 and lib.aif_cache4_scratch_ints(None) == B.ERR_ARG
+    assert lib.aif_cache4_scratch_ints(c) > 2 * 100 + 6 * 4 and lib.aif_cache4_scratch_ints(None) == B.ERR_ARG
 
 
 def test_reference_rounds_ties_to_even_codes():
