@@ -812,7 +812,7 @@ template <int OP>
 cudaError_t run_books(const BooksParams &p, cudaStream_t st)
 {
     count_launch();
-    // A few sequences: one CTA, %%% us against %%% (48 sequences of 32 pages forked), until its 32 warps have some hundred pages each.
+    // A few sequences: one CTA, 10.6 us against 12.6 (48 sequences of 32 pages forked), until its 32 warps have some hundred pages each.
     if (p.n <= kFewSeqs && (int64_t)p.n * p.c.max_pages <= 32768) {
         k_books_few<OP><<<1, kFewThreads, 0, st>>>(p);
         return cudaGetLastError();

@@ -54,14 +54,14 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_att4_rows(const AttCall a)
 
     grid_dep_wait();
     grid_dep_launch();
-    const int64_t total = plan_total(a, plan);
-    const int ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, total / a.min_units));
     const int cta = blockIdx.x;
     if (tid == 0 && a.headers) a.headers[cta].first_cta = -1;
-    if (total == 0 || cta >= ctas) return;
-    const int64_t u1 = cut(total, ctas, cta + 1);
-    int64_t u = cut(total, ctas, cta);
-    Cursor cur = plan_find(a, plan, u);
+    const Share share = plan_share(a, plan);
+    if (share.u0 >= share.u1) return;
+    const int64_t total = share.total, u1 = share.u1;
+    const int ctas = share.ctas;
+    int64_t u = share.u0;
+    Cursor cur = share.cur;
     const int d2 = d + 2;
     bool bad_page = false;
     while (u < u1) {

@@ -7,7 +7,10 @@
 // read and unpacked once where values are the keys.  The row's scale 2^E_j goes into its weight: weights are exp2(s_j + E_j - m'), with m' following
 // the largest s_j + E_j, beside the softmax's own exp2(s_j - m): fp16 weights lie in (2^-24, 2^15], and what falls below is less than 2^-31 of the largest term.  Queries are
 // held in fp16 relative to a power of two per row.  Roundings: weights to fp16 (2^-11), queries' and keys' elements below 2^-14 of their row's largest.
-// Bound: HBM, 17/32 byte per element; the products (two of 8 cycles per 256 elements and scheduler) stay below that.  Codes of the next 32 keys of a warp are in flight meanwhile.
+// Bound: the instructions that unpack, not HBM (17/32 byte per element) and not the products (two of 8 cycles per 256 elements and scheduler): a stage of 32 keys
+// costs a warp some 450, at d = 128 a quarter of them decoding, most of the rest the same for every d.  256 sequences of 10^4 rows: d = 128 50.7 us (3.4 TB/s of codes and
+// scales that are read; values are the keys), d = 256 139 us, d = 64 with values of their own 59 us.  A warp has a ring of stages in shared memory, filled by
+// asynchronous copies of whole groups; quarter rows loaded to registers by the lanes that unpack them cost more addresses: 56 us, and 195 us at d = 256.
 #include <cfloat>
 
 #include "aif_cache4_plan.cuh"
@@ -56,17 +59,17 @@ struct RowCodes {
 template <int NB>
 __device__ __forceinline__ void load_row(RowCodes<NB> &r, const uint8_t *codes, const uint8_t *scales, int t)
 {
-    if constexpr (NB == 1) r.w[0] = __ldg(reinterpret_cast<const uint32_t *>(codes) + t), r.sc[0] = __ldg(scales);
+    if constexpr (NB == 1) r.w[0] = reinterpret_cast<const uint32_t *>(codes)[t], r.sc[0] = *scales;
     if constexpr (NB == 2) {
-        const uint2 x = __ldg(reinterpret_cast<const uint2 *>(codes) + t);
-        r.w[0] = x.x, r.w[1] = x.y, r.sc[0] = __ldg(reinterpret_cast<const uint16_t *>(scales));
+        const uint2 x = reinterpret_cast<const uint2 *>(codes)[t];
+        r.w[0] = x.x, r.w[1] = x.y, r.sc[0] = *reinterpret_cast<const uint16_t *>(scales);
     }
     if constexpr (NB >= 4) {
 #pragma unroll
         for (int i = 0; i < NB / 4; ++i) {
-            const uint4 x = __ldg(reinterpret_cast<const uint4 *>(codes) + t * (NB / 4) + i);
+            const uint4 x = reinterpret_cast<const uint4 *>(codes)[t * (NB / 4) + i];
             r.w[4 * i] = x.x, r.w[4 * i + 1] = x.y, r.w[4 * i + 2] = x.z, r.w[4 * i + 3] = x.w;
-            r.sc[i] = __ldg(reinterpret_cast<const uint32_t *>(scales) + i);
+            r.sc[i] = reinterpret_cast<const uint32_t *>(scales)[i];
         }
     }
 }
@@ -80,14 +83,14 @@ __device__ __forceinline__ uint32_t top_scale(const RowCodes<NB> &r)
     if constexpr (NB == 4) return of_word(r.sc[0]);
     if constexpr (NB == 8) return max(of_word(r.sc[0]), of_word(r.sc[1]));
 }
-// fp16 pair of 2^(byte - top): 0 below 2^-24, NaN for the byte that says so.
+// fp16 pair of 2^(byte - top), 0 below 2^-24.  (The byte that stands for NaN makes the row's score NaN by itself: see row_scale.)
 __device__ __forceinline__ uint32_t relative_scale(uint32_t byte, uint32_t top)
 {
-    const uint32_t down = top - byte;
-    uint32_t h = down <= 14u ? (15u - down) << 10 : (1u << 24) >> min(down, 31u);
-    h = byte == kMxNan ? 0x7fffu : h;
-    return h | (h << 16);
+    const float f = __uint_as_float((uint32_t)max((int)(127u + byte) - (int)top, 0) << 23);
+    return pack_f16x2(f, f);
 }
+// 2^(top - 127) (the smallest is subnormal), NaN for a row that is none.
+__device__ __forceinline__ float row_scale(uint32_t top) { return __uint_as_float(top == kMxNan ? 0x7fffffffu : max(top << 23, 1u << 22)); }
 // The quarter row's values over 2^(top - 127): words 4 i .. 4 i + 3 of o are the pairs of code word i.  The lane's words t NB .. t NB + NB - 1 of the 4 NB of a row lie in
 // one block of four words, or (NB = 8) in two.
 template <int NB>
@@ -110,24 +113,38 @@ __device__ __forceinline__ void unpack_row(const RowCodes<NB> &r, uint32_t top, 
 }
 
 template <int NB, bool SHARED>
-__global__ void __launch_bounds__(kFewThreads, NB == 8 ? 2 : 3) k_att4_few(const AttCall a)
+struct FewCfg {
+    static constexpr int kGroups = NB == 8 ? 1 : 2;   // groups of 16 rows at a time: their products and exponentials overlap (one at d = 256, for want of registers)
+    static constexpr int kKinds = SHARED ? 1 : 2;
+    static constexpr int kRing = SHARED ? 6 : 4;      // stages of a warp's ring
+    static constexpr int kCodes = 16 * 16 * NB, kScales = 16 * NB;   // bytes of a group
+    static constexpr int kStage = kKinds * kGroups * (kCodes + kScales);
+    static constexpr int kBlocks = NB == 8 ? 2 : 3;   // blocks of a multiprocessor
+    static constexpr size_t kSmem = (size_t)kFewWarps * (kRing * kStage + kFewRows * (32 * NB + 2) * 4);
+};
+
+template <int NB, bool SHARED>
+__global__ void __launch_bounds__(kFewThreads, (FewCfg<NB, SHARED>::kBlocks)) k_att4_few(const AttCall a)
 {
     constexpr int D = 32 * NB, KS = 2 * NB;   // steps of 16 columns
     const Cache4 &c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    extern __shared__ float smem[];   // [warps][rows][D + 2]
+    using F = FewCfg<NB, SHARED>;
+    extern __shared__ __align__(16) unsigned char smem_dyn[];   // rings [warps][kRing][kinds][groups]: codes, then scales; sums [warps][rows][D + 2]
+    unsigned char *ring = smem_dyn + warp * F::kRing * F::kStage;
+    float *smem = reinterpret_cast<float *>(smem_dyn + kFewWarps * F::kRing * F::kStage);
     __shared__ PlanShared<kFewThreads> plan;
 
     grid_dep_wait();
     grid_dep_launch();
-    const int64_t total = plan_total(a, plan);
-    const int ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, total / a.min_units));
     const int cta = blockIdx.x;
     if (tid == 0 && a.headers) a.headers[cta].first_cta = -1;
-    if (total == 0 || cta >= ctas) return;
-    const int64_t u1 = cut(total, ctas, cta + 1);
-    int64_t u = cut(total, ctas, cta);
-    Cursor cur = plan_find(a, plan, u);
+    const Share share = plan_share(a, plan);
+    if (share.u0 >= share.u1) return;
+    const int64_t total = share.total, u1 = share.u1;
+    const int ctas = share.ctas;
+    int64_t u = share.u0;
+    Cursor cur = share.cur;
     bool bad_page = false;
     while (u < u1) {
         const Entry &e = cur.e;
@@ -139,10 +156,9 @@ __global__ void __launch_bounds__(kFewThreads, NB == 8 ? 2 : 3) k_att4_few(const
         const int32_t *table = c.table + (size_t)max(e.seq, 0) * c.max_pages;
 
         // Queries as B operand: lane (g, t) holds its quarter of the columns of row g.
-        uint32_t q[2 * KS];
+        uint32_t q[2 * KS], raw[2 * KS];
         float q_scale = 0.f;   // of row g: scale x log2(e) x the power of two that its fp16 values are relative to
         {
-            uint32_t raw[2 * KS], top = 0;
             const bool there = g < rows;
             const int rr = r0 + (there ? g : 0), query = rr / a.group;
             const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(a.q) + (e.row0 + query) * a.q_stride + (head * a.group + rr - query * a.group) * D + t * (D / 4);
@@ -151,6 +167,68 @@ __global__ void __launch_bounds__(kFewThreads, NB == 8 ? 2 : 3) k_att4_few(const
                 const uint4 x = there ? __ldg(reinterpret_cast<const uint4 *>(src) + i) : make_uint4(0u, 0u, 0u, 0u);
                 raw[4 * i] = x.x, raw[4 * i + 1] = x.y, raw[4 * i + 2] = x.z, raw[4 * i + 3] = x.w;
             }
+        }
+        // Stage n of this warp: groups first + n kStride and, if two, the one behind.  Where they lie and what of them is visible is worked out for 32 groups at a time, one to
+        // a lane, a batch ahead; codes and scales come kRing - 1 stages ahead, by asynchronous copies: a group is one piece of each.
+        constexpr int G = F::kGroups, kStride = kFewWarps * G;
+        const int first = g0 + warp * G, stages = first < g1 ? (g1 - first + kStride - 1) / kStride : 0;
+        struct Batch {
+            int32_t page;            // of this lane's group
+            uint32_t in_pages, span; // groups before it in a page (all heads), its visible rows: [span & 255, span >> 8)
+        };
+        auto load_batch = [&](int n) {
+            const int gi = min(first + (n + lane / G) * kStride + lane % G, g1 - 1);   // (behind the last group: that one again, of which nothing is visible)
+            const bool sink = gi < sink_groups, there = gi == first + (n + lane / G) * kStride + lane % G;
+            const int row = (sink ? gi : gi + rest_group) << 4;
+            const int lo = sink ? 0 : max(e.rest - row, 0), hi = there ? min(16, (sink ? e.first : e.length) - row) : 0;
+            return Batch{__ldg(table + (row >> c.page_shift)), (uint32_t)((head << c.page_shift) + (row & (c.page_rows() - 1))) >> 4, (uint32_t)lo | (uint32_t)hi << 8};
+        };
+        const uint32_t page_groups = (uint32_t)(c.heads << c.page_shift) >> 4;
+        // the groups' places in the pool, in groups; those of pages that do not exist are marked in the span and read page 0
+        uint32_t place = 0, span = 0;
+        Batch ahead{};
+        auto settle = [&](const Batch &b) {
+            const bool ok = c.holds(b.page);
+            bad_page |= !ok;
+            place = (ok ? (uint32_t)b.page : 0u) * page_groups + b.in_pages, span = b.span | (ok ? 0u : 1u << 16);
+        };
+        if (stages > 0) settle(load_batch(0));
+        if (stages > 32 / G) ahead = load_batch(32 / G);
+        const uint32_t ring_at = smem_u32(ring) + lane * 16;
+        const uint8_t *codes_at[F::kKinds], *scales_at[F::kKinds];
+#pragma unroll
+        for (int k = 0; k < F::kKinds; ++k) codes_at[k] = c.codes[k] + lane * 16, scales_at[k] = c.scales[k] + lane * 16;
+        int slot_in = 0;
+        uint32_t span_now = span, span_next = 0;   // spans of the batch that is at work (copies may be in the next one already)
+        auto bring = [&](int n) {
+            if (n < stages) {
+                if (n > 0 && n % (32 / G) == 0) {
+                    settle(ahead);
+                    span_next = span;
+                    if (n + 32 / G < stages) ahead = load_batch(n + 32 / G);
+                }
+                const uint32_t to0 = ring_at + (uint32_t)(slot_in * F::kStage);
+#pragma unroll
+                for (int x = 0; x < G; ++x) {
+                    const uint32_t at = __shfl_sync(0xffffffffu, place, (n * G + x) & 31);
+#pragma unroll
+                    for (int k = 0; k < F::kKinds; ++k) {
+                        const uint32_t to = to0 + (uint32_t)((k * G + x) * (F::kCodes + F::kScales));
+                        const uint8_t *codes = codes_at[k] + (size_t)at * F::kCodes;
+#pragma unroll
+                        for (int y = 0; y < (NB + 1) / 2; ++y)
+                            if (NB > 1 || lane < 16) cp_async16(to + y * 512, codes + y * 512, 16u);
+                        if (lane < NB) cp_async16(to + F::kCodes, scales_at[k] + (size_t)at * F::kScales, 16u);
+                    }
+                }
+                slot_in = slot_in + 1 == F::kRing ? 0 : slot_in + 1;
+            }
+            cp_async_commit();
+        };
+#pragma unroll 1
+        for (int n = 0; n < F::kRing - 1; ++n) bring(n);
+        {
+            uint32_t top = 0;
 #pragma unroll
             for (int i = 0; i < 2 * KS; ++i) top = max(top, max(raw[i] & 0x7fffu, (raw[i] >> 16) & 0x7fffu));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -169,113 +247,101 @@ __global__ void __launch_bounds__(kFewThreads, NB == 8 ? 2 : 3) k_att4_few(const
         for (int s = 0; s < KS; ++s) o[s][0] = o[s][1] = o[s][2] = o[s][3] = 0.f;
         float m[2] = {-FLT_MAX, -FLT_MAX}, mw[2] = {-FLT_MAX, -FLT_MAX}, l[2] = {0.f, 0.f};   // offsets of the weights' sum and of the values', per row
 
-        RowCodes<NB> kn[2][2], vn[SHARED ? 1 : 2][2];   // [group][key g, key g + 8]
-        // a lane's piece of row g of a page's group: from here, page strides and rows further
-        const uint32_t page_codes = (uint32_t)(c.heads << c.page_shift) * (D / 2), page_scales = (uint32_t)(c.heads << c.page_shift) * NB;
-        const size_t head_row = ((size_t)head << c.page_shift) + g;
-        auto fetch = [&](int grp) {   // codes of the groups grp and grp + 1
+        int slot = 0;
+        for (int n = 0; n < stages; ++n) {
+            if (n > 0 && n % (32 / G) == 0) span_now = span_next;
+            bring(n + F::kRing - 1);   // (into the slot that was read a stage ago)
+            cp_async_wait<F::kRing - 1>();
+            __syncwarp();
+            const unsigned char *stage = ring + slot * F::kStage + g * (D / 2), *stage_sc = ring + slot * F::kStage + F::kCodes + g * NB;
+            slot = slot + 1 == F::kRing ? 0 : slot + 1;
+            uint32_t kf[G][2][4 * NB];                       // keys (then values) as fp16 pairs
+            RowCodes<NB> vc[SHARED ? 1 : G][2];
+            float scale[G][2], s[G][4], w[G][4], v_exp[G][2];
+            bool see[G][2];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const int gi = min(grp + x, g1 - 1);   // (an odd last one is read twice and used once)
-                const int row = (gi < sink_groups ? gi : gi + rest_group) << 4;
-                int page = __ldg(table + (row >> c.page_shift));
-                const bool ok = c.holds(page);
-                bad_page |= !ok;
-                page = ok ? page : 0;
-                const size_t at = head_row + (row & (c.page_rows() - 1));
-                const size_t codes = (size_t)(uint32_t)page * page_codes + at * (D / 2), scales = (size_t)(uint32_t)page * page_scales + at * NB;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    load_row<NB>(kn[x][h], c.codes[0] + codes + h * 8 * (D / 2), c.scales[0] + scales + h * 8 * NB, t);
-                    if constexpr (!SHARED) load_row<NB>(vn[x][h], c.codes[1] + codes + h * 8 * (D / 2), c.scales[1] + scales + h * 8 * NB, t);
-                    if (!ok) {   // no such page: no number
-#pragma unroll
-                        for (int i = 0; i < (NB + 3) / 4; ++i) kn[x][h].sc[i] = NB == 1 ? 0xffu : NB == 2 ? 0xffffu : 0xffffffffu;
-                    }
-                }
-            }
-        };
-        int grp = g0 + warp * 2;
-        if (grp < g1) fetch(grp);
-        for (; grp < g1; grp += kFewWarps * 2) {
-            RowCodes<NB> kc[2][2], vc[SHARED ? 1 : 2][2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int x = 0; x < G; ++x) {
+                const uint32_t sp = __shfl_sync(0xffffffffu, span_now, (n * G + x) & 31), lo = sp & 255u, hi = (sp >> 8) & 255u;
+                RowCodes<NB> kr[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    kc[x][h] = kn[x][h];
-                    if constexpr (!SHARED) vc[x][h] = vn[x][h];
+                    load_row<NB>(kr[h], stage + x * (F::kCodes + F::kScales) + 8 * h * (D / 2), stage_sc + x * (F::kCodes + F::kScales) + 8 * h * NB, t);
+                    if constexpr (!SHARED)
+                        load_row<NB>(vc[x][h], stage + (G + x) * (F::kCodes + F::kScales) + 8 * h * (D / 2), stage_sc + (G + x) * (F::kCodes + F::kScales) + 8 * h * NB, t);
+                    see[x][h] = g + 8 * h >= lo && g + 8 * h < hi;
                 }
-            if (grp + kFewWarps * 2 < g1) fetch(grp + kFewWarps * 2);
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                if (grp + x >= g1) break;
-                const int gi = grp + x;
-                const bool sink = gi < sink_groups;
-                const int row = (sink ? gi : gi + rest_group) << 4;
-                const int lo = sink ? 0 : e.rest, hi = sink ? e.first : e.length;   // visible rows of the group: [lo, hi)
-                const bool see[2] = {row + g >= lo && row + g < hi, row + g + 8 >= lo && row + g + 8 < hi};
-                if (row < lo || row + 16 > hi) {
-                    // rows that are not visible have no scale, whatever stands there (codes are finite)
+                if (sp != 16u << 8) {
+                    // rows that are not visible have no scale, whatever stands there (codes are finite); those of a page that does not exist are no numbers
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        if (!see[h]) {
 #pragma unroll
-                            for (int i = 0; i < (NB + 3) / 4; ++i) {
-                                kc[x][h].sc[i] = 0u;
-                                if constexpr (!SHARED) vc[x][h].sc[i] = 0u;
-                            }
+                        for (int i = 0; i < (NB + 3) / 4; ++i) {
+                            const uint32_t bad = NB == 1 ? 0xffu : NB == 2 ? 0xffffu : 0xffffffffu;
+                            kr[h].sc[i] = !see[x][h] ? 0u : sp >> 16 ? bad : kr[h].sc[i];
+                            if constexpr (!SHARED) vc[x][h].sc[i] = !see[x][h] ? 0u : vc[x][h].sc[i];
                         }
                 }
-                uint32_t top[2] = {top_scale<NB>(kc[x][0]), top_scale<NB>(kc[x][1])};
-                uint32_t ka[4 * NB], kb[4 * NB];
-                unpack_row<NB>(kc[x][0], top[0], t, ka);
-                unpack_row<NB>(kc[x][1], top[1], t, kb);
-                float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < KS; ++i) mma_f16(s, ka[2 * i], kb[2 * i], ka[2 * i + 1], kb[2 * i + 1], q[2 * i], q[2 * i + 1]);
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t top = top_scale<NB>(kr[h]);
+                    unpack_row<NB>(kr[h], top, t, kf[x][h]);
+                    scale[x][h] = row_scale(top);
+                    // the exponent of the values' scale; a row of no numbers is one in its weights
+                    uint32_t vtop = top;
+                    if constexpr (!SHARED) vtop = top_scale<NB>(vc[x][h]);
+                    v_exp[x][h] = !SHARED && vtop == kMxNan ? NAN : (float)(int)vtop;
+                }
+            }
+            bool raise = false;
+#pragma unroll
+            for (int x = 0; x < G; ++x) {
+                float s2[2][4] = {};   // two chains of products
+#pragma unroll
+                for (int i = 0; i < KS; ++i) mma_f16(s2[i & 1], kf[x][0][2 * i], kf[x][1][2 * i], kf[x][0][2 * i + 1], kf[x][1][2 * i + 1], q[2 * i], q[2 * i + 1]);
                 // s[0], s[1]: key g, rows 2 t, 2 t + 1; s[2], s[3]: key g + 8
-                const float scale[2] = {mx_scale(top[0]), mx_scale(top[1])};
-                uint32_t vtop[2] = {top[0], top[1]};
-                if constexpr (!SHARED) vtop[0] = top_scale<NB>(vc[x][0]), vtop[1] = top_scale<NB>(vc[x][1]);
-                float w[4];
-                bool raise = false;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    s[i] = see[i >> 1] ? s[i] * (k2[i & 1] * scale[i >> 1]) : -INFINITY;
-                    w[i] = s[i] + (float)((int)vtop[i >> 1] - 127);
-                    raise |= s[i] > m[i & 1] + 8.f || w[i] > mw[i & 1] + 8.f;
+                    s[x][i] = see[x][i >> 1] ? (s2[0][i] + s2[1][i]) * (k2[i & 1] * scale[x][i >> 1]) : -INFINITY;
+                    w[x][i] = s[x][i] + v_exp[x][i >> 1];
+                    raise |= s[x][i] > m[i & 1] + 8.f || w[x][i] > mw[i & 1] + 8.f;
                 }
-                // the offsets follow the maxima only when those have grown by a factor of 2^8
-                if (__any_sync(0xffffffffu, raise)) {
+            }
+            // the offsets follow the maxima only when those have grown by a factor of 2^8
+            if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        float ms = fmaxf(s[r], s[r + 2]), mv = fmaxf(w[r], w[r + 2]);
+                for (int r = 0; r < 2; ++r) {
+                    float ms = -FLT_MAX, mv = -FLT_MAX;
 #pragma unroll
-                        for (int b = 4; b < 32; b <<= 1) ms = fmaxf(ms, __shfl_xor_sync(0xffffffffu, ms, b)), mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, b));
-                        ms = ms > m[r] + 8.f ? ms : m[r], mv = mv > mw[r] + 8.f ? mv : mw[r];
-                        const float f = fast_exp2(mw[r] - mv);
-                        l[r] *= fast_exp2(m[r] - ms);
-                        m[r] = ms, mw[r] = mv;
+                    for (int x = 0; x < G; ++x) ms = fmaxf(ms, fmaxf(s[x][r], s[x][r + 2])), mv = fmaxf(mv, fmaxf(w[x][r], w[x][r + 2]));
 #pragma unroll
-                        for (int i = 0; i < KS; ++i) o[i][r] *= f, o[i][r + 2] *= f;
-                    }
+                    for (int b = 4; b < 32; b <<= 1) ms = fmaxf(ms, __shfl_xor_sync(0xffffffffu, ms, b)), mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, b));
+                    ms = ms > m[r] + 8.f ? ms : m[r], mv = mv > mw[r] + 8.f ? mv : mw[r];
+                    const float f = fast_exp2(mw[r] - mv);
+                    l[r] *= fast_exp2(m[r] - ms);
+                    m[r] = ms, mw[r] = mv;
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) o[i][r] *= f, o[i][r + 2] *= f;
                 }
+            }
+            const float mb[2] = {kWeightBias - mw[0], kWeightBias - mw[1]};
+#pragma unroll
+            for (int x = 0; x < G; ++x) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    l[i & 1] += fast_exp2(s[i] - m[i & 1]);
-                    w[i] = fast_exp2(w[i] - mw[i & 1] + kWeightBias);
+                    l[i & 1] += fast_exp2(s[x][i] - m[i & 1]);
+                    w[x][i] = fast_exp2(w[x][i] + mb[i & 1]);
                 }
-                const uint32_t p0 = transpose8(pack_f16x2(w[0], w[1])), p1 = transpose8(pack_f16x2(w[2], w[3]));
+                const uint32_t p0 = transpose8(pack_f16x2(w[x][0], w[x][1])), p1 = transpose8(pack_f16x2(w[x][2], w[x][3]));
                 if constexpr (!SHARED) {
-                    unpack_row<NB>(vc[x][0], vtop[0], t, ka);
-                    unpack_row<NB>(vc[x][1], vtop[1], t, kb);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) unpack_row<NB>(vc[x][h], top_scale<NB>(vc[x][h]), t, kf[x][h]);
                 }
 #pragma unroll
                 for (int i = 0; i < KS; ++i)
-                    mma_f16(o[i], transpose8(ka[2 * i]), transpose8(ka[2 * i + 1]), transpose8(kb[2 * i]), transpose8(kb[2 * i + 1]), p0, p1);
+                    mma_f16(o[i], transpose8(kf[x][0][2 * i]), transpose8(kf[x][0][2 * i + 1]), transpose8(kf[x][1][2 * i]), transpose8(kf[x][1][2 * i + 1]), p0, p1);
             }
         }
+        cp_async_wait_all();
         // O^T: o[i][0], [1]: rows 2 t, 2 t + 1 of the column that lane quarter g / 2 has as element g % 2 of its pair 2 i; o[i][2], [3]: of its pair 2 i + 1
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -283,7 +349,7 @@ __global__ void __launch_bounds__(kFewThreads, NB == 8 ? 2 : 3) k_att4_few(const
 #pragma unroll
             for (int b = 4; b < 32; b <<= 1) lt += __shfl_xor_sync(0xffffffffu, lt, b);
             float *to = smem + (warp * kFewRows + 2 * t + r) * (D + 2);
-            const float f = fast_exp2(mw[r] - kWeightBias - m[r]);   // sums relative to the offset of the weights' sum
+            const float f = fast_exp2(mw[r] - kWeightBias - 127.f - m[r]);   // sums relative to the offset of the weights' sum
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 const int col = (g >> 1) * (D / 4) + (g & 1) + 4 * i;
@@ -302,7 +368,7 @@ __global__ void __launch_bounds__(kFewThreads, NB == 8 ? 2 : 3) k_att4_few(const
 #pragma unroll
             for (int w = 0; w < kFewWarps; ++w) {
                 const float *from = smem + (w * kFewRows + r) * (D + 2);
-                if (g0 + w * 2 < g1) {   // (a warp without keys has nothing to say)
+                if (g0 + w * G < g1) {   // (a warp without keys has nothing to say)
                     const float f = fast_exp2(from[D] - mt);
                     sum += from[col] * f, weight += from[D + 1] * f;
                 }
@@ -335,11 +401,9 @@ __global__ void __launch_bounds__(kFewThreads, NB == 8 ? 2 : 3) k_att4_few(const
 template <int NB, bool SHARED>
 cudaError_t run_few(const AttCall &a, int grid, cudaStream_t st)
 {
-    const size_t smem = (size_t)kFewWarps * kFewRows * (32 * NB + 2) * 4;   // up to 65 KB
-    if (smem > 48 * 1024) {
-        const cudaError_t e = allow_smem<k_att4_few<NB, SHARED>>(smem);
-        if (e != cudaSuccess) return e;
-    }
+    const size_t smem = FewCfg<NB, SHARED>::kSmem;
+    const cudaError_t e = allow_smem<k_att4_few<NB, SHARED>>(smem);
+    if (e != cudaSuccess) return e;
     count_launch();
     return launch_pdl(k_att4_few<NB, SHARED>, dim3(grid), dim3(kFewThreads), smem, st, a);
 }

@@ -81,13 +81,13 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
     grid_dep_wait();
     grid_dep_launch();
 
-    const int64_t total = plan_total(a, plan);
-    const int ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, total / a.min_units)), cta = blockIdx.x;
+    const int cta = blockIdx.x;
     if (tid == 0 && a.headers) a.headers[cta].first_cta = -1;
-    const bool work = total > 0 && cta < ctas;
-    const int64_t u0 = work ? cut(total, ctas, cta) : 0, u1 = work ? cut(total, ctas, cta + 1) : 0;
-    Cursor cur{};
-    if (work) cur = plan_find(a, plan, u0);
+    const Share share = plan_share(a, plan);
+    const int64_t total = share.total, u0 = share.u0, u1 = share.u1;
+    const int ctas = share.ctas;
+    const bool work = u0 < u1;
+    Cursor cur = share.cur;
     int64_t u = u0;
     auto tile_of = [&](const Cursor &at, int &head, int &r0, int &rows) {
         const int row_tiles = at.tiles / c.heads;

@@ -91,31 +91,62 @@ struct Cursor {
 // Shared memory of the division.
 template <int THREADS>
 struct PlanShared {
-    int64_t sum[THREADS];   // units before the entries of every thread
-    int64_t total;
-    int32_t bad;
+    int64_t sum[THREADS];   // units before the sequences of every thread
 };
 
-__device__ __forceinline__ int64_t cut(int64_t total, int ctas, int c) { return total / ctas * c + total % ctas * c / ctas; }
-
-// All threads.  Returns the units of the call (0 with *bad: offsets that cannot be) and the number of CTAs that get any; on return sum[t] holds the
-// units before the entries of thread t.
-template <int THREADS>
-__device__ int64_t plan_total(const AttCall &a, PlanShared<THREADS> &s)
+// x / y for y > 0: in 32 bits where that does (a 64-bit division costs some hundred cycles).
+__device__ __forceinline__ int64_t divide(int64_t x, int64_t y)
 {
-    const int tid = threadIdx.x, lane = tid & 31;
-    const int per = (a.n + THREADS - 1) / THREADS;
-    int64_t mine = 0;
+    if (((x | y) >> 32) == 0) return (uint32_t)x / (uint32_t)y;
+    return x / y;
+}
+// First unit of CTA c of `ctas`: an even share of `total`.
+__device__ __forceinline__ int64_t cut(int64_t total, int ctas, int c)
+{
+    if (total < (int64_t)1 << 22) return (uint32_t)total * (uint32_t)c / (uint32_t)ctas;   // (ctas <= 444)
+    const int64_t each = divide(total, ctas);
+    return each * c + divide((total - each * ctas) * c, ctas);
+}
+
+// What a CTA of the launch has to do: the units [u0, u1), the first of them at `cur`.  total 0: nothing for anybody.
+struct Share {
+    int64_t total, u0, u1;
+    int32_t ctas;
+    Cursor cur;
+};
+
+__device__ __forceinline__ bool offsets_ok(const AttCall &a, int i)
+{
+    if (!a.offsets) return true;
+    const int64_t o = a.offsets[i], o1 = a.offsets[i + 1];
+    return o >= 0 && o1 >= o && o1 <= a.rows;
+}
+
+// All threads.  Up to 128 sequences every warp works it out by itself, four to a lane; beyond that the threads of the CTA share them.
+template <int THREADS>
+__device__ Share plan_share(const AttCall &a, PlanShared<THREADS> &s)
+{
+    const int tid = threadIdx.x, lane = tid & 31, cta = blockIdx.x;
+    const bool few = a.n <= 128;
+    const int per = few ? (a.n + 31) >> 5 : (a.n + THREADS - 1) / THREADS, first = (few ? lane : tid) * per;
+    int64_t mine = 0, unit[4] = {0, 0, 0, 0};
     bool bad = false;
-    for (int i = tid * per; i < min(a.n, (tid + 1) * per); ++i) {
-        if (a.offsets) {
-            const int64_t o = a.offsets[i], o1 = a.offsets[i + 1];
-            if (o < 0 || o1 < o || o1 > a.rows) {
-                bad = true;
-                continue;
+    if (few) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = first + j;
+            if (j < per && i < a.n) {
+                if (offsets_ok(a, i)) unit[j] = units_at(a, entry_at(a, i));
+                else bad = true;
             }
+            mine += unit[j];
         }
-        mine += units_at(a, entry_at(a, i));
+    } else {
+#pragma unroll 4
+        for (int i = first; i < min(a.n, first + per); ++i) {
+            if (offsets_ok(a, i)) mine += units_at(a, entry_at(a, i));
+            else bad = true;
+        }
     }
     int64_t x = mine;
 #pragma unroll
@@ -123,46 +154,63 @@ __device__ int64_t plan_total(const AttCall &a, PlanShared<THREADS> &s)
         const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
         if (lane >= o) x += y;
     }
-    __shared__ int64_t warp_sum[THREADS / 32];
-    if (lane == 31) warp_sum[tid >> 5] = x;
-    const bool any_bad = __syncthreads_or(bad) != 0;
-    int64_t base = 0, all = 0;
-    for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < (tid >> 5)) base += warp_sum[w];
-        all += warp_sum[w];
+    int64_t base = x - mine;
+    Share h;
+    if (few) {
+        h.total = __shfl_sync(0xffffffffu, x, 31);
+        bad = __any_sync(0xffffffffu, bad);
+    } else {
+        __shared__ int64_t warp_sum[THREADS / 32];
+        if (lane == 31) warp_sum[tid >> 5] = x;
+        bad = __syncthreads_or(bad) != 0;
+        int64_t before = 0;
+        h.total = 0;
+        for (int w = 0; w < THREADS / 32; ++w) {
+            if (w < (tid >> 5)) before += warp_sum[w];
+            h.total += warp_sum[w];
+        }
+        base += before;
+        s.sum[tid] = base;
+        __syncthreads();
     }
-    s.sum[tid] = base + x - mine;
-    __syncthreads();
-    if (any_bad) {
-        if (tid == 0 && blockIdx.x == 0) atomicOr(a.c.status, AIF_STATUS_BAD_ID);
-        return 0;
+    h.u0 = h.u1 = 0, h.ctas = 1, h.cur = Cursor{};
+    if (bad) {
+        h.total = 0;
+        if (tid == 0 && cta == 0) atomicOr(a.c.status, AIF_STATUS_BAD_ID);
     }
-    return all;
-}
-
-// The place of unit u (u < total); any thread, after plan_total.
-template <int THREADS>
-__device__ Cursor plan_find(const AttCall &a, const PlanShared<THREADS> &s, int64_t u)
-{
-    int lo = 0, hi = THREADS;   // the last thread whose entries begin at or before u
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s.sum[mid] <= u) lo = mid;
-        else hi = mid;
+    if (h.total == 0) return h;
+    h.ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, a.min_units == 1 ? h.total : divide(h.total, a.min_units)));
+    if (cta >= h.ctas) return h;
+    h.u0 = cut(h.total, h.ctas, cta), h.u1 = cut(h.total, h.ctas, cta + 1);
+    // the sequence of unit u0
+    int i;
+    int64_t left;
+    if (few) {
+        left = h.u0 - base, i = first;
+        const int who = __ffs(__ballot_sync(0xffffffffu, left >= 0 && left < mine)) - 1;
+#pragma unroll
+        for (int j = 0; j < 3; ++j)
+            if (i == first + j && left >= unit[j]) left -= unit[j], ++i;
+        i = __shfl_sync(0xffffffffu, i, who), left = __shfl_sync(0xffffffffu, left, who);
+    } else {
+        int lo = 0, hi = THREADS;   // the last thread whose sequences begin at or before u0
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (s.sum[mid] <= h.u0) lo = mid;
+            else hi = mid;
+        }
+        i = lo * per, left = h.u0 - s.sum[lo];
+        for (; i < a.n - 1; ++i) {
+            const int64_t has = units_at(a, entry_at(a, i));
+            if (left < has) break;
+            left -= has;
+        }
     }
-    const int per = (a.n + THREADS - 1) / THREADS;
-    Cursor c;
-    c.i = lo * per;
-    int64_t left = u - s.sum[lo];
-    for (;; ++c.i) {
-        c.e = entry_at(a, c.i);
-        const int64_t has = units_at(a, c.e);
-        if (left < has || c.i >= a.n - 1) break;
-        left -= has;
-    }
+    Cursor &c = h.cur;
+    c.i = i, c.e = entry_at(a, i);
     c.tiles = tiles_at(a, c.e) * a.c.heads, c.blocks = blocks_at(a, c.e);
-    c.tile = (int)(left / c.blocks), c.block = (int)(left - (int64_t)c.tile * c.blocks);
-    return c;
+    c.tile = (int)divide(left, c.blocks), c.block = (int)(left - (int64_t)c.tile * c.blocks);
+    return h;
 }
 // To the next tile (block 0 of it).
 __device__ __forceinline__ void plan_next(const AttCall &a, Cursor &c)
