@@ -60,7 +60,8 @@ def check_rows(c, model, values):
         assert torch.equal(o.double(), v[tags])
 
 
-@pytest.mark.parametrize("seed, n_seqs, heads, shared, page_rows, d", [(0, 5, 1, True, 16, 32), (1, 40, 2, False, 16, 64), (2, 9, 1, True, 32, 128), (3, 70, 1, False, 16, 96)])
+@pytest.mark.parametrize("seed, n_seqs, heads, shared, page_rows, d", [(0, 5, 1, True, 16, 32), (1, 40, 2, False, 16, 64), (2, 9, 1, True, 32, 128), (3, 70, 1, False, 16, 96), (4, 200, 1, True, 16, 32),
+                                                                  (5, 1100, 1, True, 16, 32)])
 def test_books_against_the_model(seed, n_seqs, heads, shared, page_rows, d):
     """Random appends, forks, copies, frees and compactions, duplicates, bad ids and full caches among them."""
     rng = random.Random(seed)
@@ -68,7 +69,8 @@ def test_books_against_the_model(seed, n_seqs, heads, shared, page_rows, d):
     c = B.Cache4(d=d, n_pages=n_pages, page_rows=page_rows, n_seqs=n_seqs, max_pages=max_pages, heads=heads, shared=shared)
     model = R.Books(n_pages, page_rows, n_seqs, max_pages)
     g = torch.Generator(device="cuda").manual_seed(seed)
-    stock = [torch.randn(4000, heads, d, generator=g, device="cuda").bfloat16() for _ in range(1 if shared else 2)]
+    n_stock = max(4000, (2 * page_rows + 5) * n_seqs)
+    stock = [torch.randn(n_stock, heads, d, generator=g, device="cuda").bfloat16() for _ in range(1 if shared else 2)]
     values = [R.quantise(x)[0] for x in stock]
     used = 0
 
@@ -84,7 +86,7 @@ def test_books_against_the_model(seed, n_seqs, heads, shared, page_rows, d):
         if op == "append":
             who = some()
             counts = [rng.choice([0, 1, 3, page_rows - 1, page_rows, page_rows + 5, rng.randint(0, 2 * page_rows)]) for _ in who]
-            if used + sum(counts) > 4000:
+            if used + sum(counts) > n_stock:
                 used = 0
             tags = list(range(used, used + sum(counts)))
             c.append(ids(*who), offsets(counts), *[x[used:used + sum(counts)] for x in stock])
@@ -111,6 +113,32 @@ def test_books_against_the_model(seed, n_seqs, heads, shared, page_rows, d):
             model.share(src, dst, op == "copy")
         check_books(c, model)
         assert c.poll_status() == (B.STATUS_BAD_ID if model.bad else 0) | (B.STATUS_FULL if model.full else 0), (step, op)
+    check_rows(c, model, values)
+
+
+def test_books_of_long_tables():
+    """Few sequences whose tables are longer than what one CTA goes through."""
+    c = B.Cache4(d=32, n_pages=2100, page_rows=16, n_seqs=4, max_pages=20000)
+    model = R.Books(2100, 16, 4, 20000)
+    rows = torch.randn(33000, 1, 32, device="cuda").bfloat16()
+    values = [R.quantise(rows)[0]]
+    c.append(ids(2, 0), offsets([30000, 1500]), rows[:31500])
+    model.append([2, 0], [30000, 1500], list(range(31500)))
+    check_books(c, model)
+    c.fork(ids(2, 0), ids(1, 3))
+    model.share([2, 0], [1, 3], False)
+    c.append(ids(1, 3, 2), offsets([20, 700, 0]), rows[31500:32220])
+    model.append([1, 3, 2], [20, 700, 0], list(range(31500, 32220)))
+    check_books(c, model)
+    check_rows(c, model, values)
+    c.free(ids(2, 3))
+    model.free_seqs([2, 3])
+    check_books(c, model)
+    c.append(ids(2), offsets([33000]), rows)   # 2063 pages: there are not as many left
+    model.full = False
+    model.append([2], [33000], list(range(33000)))
+    assert model.full and c.poll_status() == B.STATUS_FULL
+    check_books(c, model)
     check_rows(c, model, values)
 
 
@@ -338,6 +366,23 @@ def test_many_sequences():
         out = c.attention(q.to(dtype), torch.empty(n, 1, 32, dtype=dtype, device="cuda"))
         for i in range(0, n, 97):
             check_attention(c, [k[i]], [v[i]], q.to(dtype)[i:i + 1], [1], [0], out[i:i + 1])
+
+
+@pytest.mark.parametrize("n", [128, 129, 700])
+@pytest.mark.parametrize("dtype, d", [(torch.float32, 64), (torch.bfloat16, 128)])
+def test_bad_offsets_anywhere(n, dtype, d):
+    c, k, v = filled([(11 * i) % 60 for i in range(n)], d, page_rows=16)
+    q = (torch.randn(2 * n, 1, d, device="cuda") * 8).to(dtype)
+    off = offsets([2] * n)
+    for at, value in ((0, -1), (n // 2, 0), (n - 1, 2 * n + 1), (n, 2 * n + 1)):
+        bad, out = off.clone(), torch.full_like(q, 7.0)
+        bad[at] = value
+        c.attention(q, out, offsets=bad)
+        assert (out == 7).all() and c.poll_status() == B.STATUS_BAD_ID, (at, value)
+    out = c.attention(q, torch.empty_like(q), offsets=off)
+    assert c.poll_status() == 0
+    for i in range(0, n, 61):
+        check_attention(c, [k[i]], [v[i]], q[2 * i:2 * i + 2], [2], [0], out[2 * i:2 * i + 2])
 
 
 def test_pages_behind_four_gigabytes():
