@@ -81,6 +81,82 @@ struct GemmParams {
     uint32_t *status;
 };
 
+// 32 rows x 64 columns of an accumulator, by one warp: from tensor memory through shared memory (two slabs of 4 KB) to `out`, in pieces of 128 bytes of a row, swizzled
+// so that the lanes (one row each) stay on different banks and a tile store takes them in the same form.  `freed` is told once the accumulator has been read.
+template <typename T>
+__device__ __forceinline__ void store_half(const GemmParams &p, const CUtensorMap &tmO, uint32_t src, int64_t row0, int n0, unsigned char *slabs, int &slab, const float *bias_s,
+                                           uint32_t freed)
+{
+    constexpr int kCols = 128 / (int)sizeof(T);   // columns of a piece
+    constexpr int kPer = 16 / (int)sizeof(T);     // elements of 16 bytes
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int c0 = 0; c0 < 64; c0 += 32) {
+        uint32_t r[32];
+        tmem_ld32(src + c0, r);
+        tmem_ld_wait();
+        if (c0 == 32) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(freed);
+        }
+        const int first = c0 / kCols * kCols, col = n0 + first;   // of the piece that these columns lie in
+        unsigned char *sb = slabs + slab * 4096;
+        if (c0 == first) {
+            if (p.wide && lane == 0) bulk_wait_read<1>();   // the store that last read this slab is done with it
+            __syncwarp();
+        }
+#pragma unroll
+        for (int q = 0; q < 32 / kPer; ++q) {
+            float v[kPer];
+#pragma unroll
+            for (int i = 0; i < kPer; i += 4) {
+                const float4 bb = *reinterpret_cast<const float4 *>(bias_s + c0 + q * kPer + i);
+                const float add[4] = {bb.x, bb.y, bb.z, bb.w};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    v[i + x] = __uint_as_float(r[q * kPer + i + x]) + add[x];
+                    if (p.relu) v[i + x] = v[i + x] < 0.f ? 0.f : v[i + x];   // NaN stays
+                }
+            }
+            uint4 o;
+            if constexpr (sizeof(T) == 2) {
+                uint32_t pk[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const __nv_bfloat162 hh = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                    pk[i] = *reinterpret_cast<const uint32_t *>(&hh);
+                }
+                o = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+            } else {
+                o = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+            }
+            *reinterpret_cast<uint4 *>(sb + lane * 128 + (((q + (c0 - first) / kPer) ^ (lane & 7)) << 4)) = o;
+        }
+        if (c0 + 32 < first + kCols) continue;
+        if (p.wide) {
+            // rows and columns behind the end are not stored
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+                if (row0 < p.m && col < p.n) tma_store_2d(&tmO, smem_u32(sb), col, (int)row0);
+                bulk_commit();
+            }
+            slab ^= 1;
+        } else {
+            __syncwarp();
+            // a row at a time, a lane to an element
+            T *out = static_cast<T *>(p.out);
+            for (int rr = 0; rr < 32 && row0 + rr < p.m; ++rr) {
+#pragma unroll
+                for (int x = lane; x < kCols; x += 32)
+                    if (col + x < p.n) out[(row0 + rr) * p.out_stride + col + x] = *reinterpret_cast<const T *>(sb + rr * 128 + ((x / kPer ^ (rr & 7)) << 4) + x % kPer * sizeof(T));
+            }
+            __syncwarp();
+        }
+    }
+}
+
 template <typename T>
 __global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                                                                        const __grid_constant__ CUtensorMap tmO, const GemmParams p)
@@ -172,9 +248,7 @@ __global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_
             if (ok) umma_commit_if(one, smem_u32(acc_full + b));
         }
     } else if (warp >= 4) {
-        // Two warps to a quarter of the rows, each with half of the columns: pieces of 128 bytes of a row, swizzled in shared memory so that the
-        // lanes (one row each) stay on different banks and a tile store takes them in the same form.
-        constexpr int kCols = 128 / (int)sizeof(T);   // columns of a piece
+        // two warps to a quarter of the rows, each with half of the columns
         const int w = (warp - 4) & 3, half = (warp - 4) >> 2;
         unsigned char *stg = smOut + (warp - 4) * 2 * 4096;
         float *bias_s = reinterpret_cast<float *>(smOut + C::kOutBytes + 256) + (warp - 4) * 64;
@@ -187,72 +261,9 @@ __global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_
 #pragma unroll
             for (int x = 0; x < 64; x += 32) bias_s[x + lane] = p.bias && n0 + x + lane < p.n ? __ldg(p.bias + n0 + x + lane) : 0.f;
             __syncwarp();
-            if (!mbar_wait(smem_u32(acc_full + b), (uint32_t)((t >> 1) & 1), abort_flag)) break;
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(acc_full + b), (uint32_t)((t >> 1) & 1), abort_flag))) break;
             tc_fence_after();
-            uint32_t r[64];
-            const uint32_t src = tmem + ((uint32_t)(w * 32) << 16) + (uint32_t)(b * 128 + half * 64);
-            tmem_ld32(src, *reinterpret_cast<uint32_t(*)[32]>(&r[0]));
-            tmem_ld32(src + 32, *reinterpret_cast<uint32_t(*)[32]>(&r[32]));
-            tmem_ld_wait();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(acc_empty + b));   // in registers: the accumulator is free
-#pragma unroll
-            for (int c0 = 0; c0 < 64; c0 += kCols) {
-                const int col = n0 + c0;
-                if (col >= p.n) break;
-                unsigned char *sb = stg + slab * 4096;
-                if (p.wide && lane == 0) bulk_wait_read<1>();   // the store that last read this slab is done with it
-                __syncwarp();
-                constexpr int kPer = 16 / (int)sizeof(T);       // elements of 16 bytes
-#pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    float v[kPer];
-#pragma unroll
-                    for (int i = 0; i < kPer; i += 4) {
-                        const float4 bb = *reinterpret_cast<const float4 *>(bias_s + c0 + q * kPer + i);
-                        const float add[4] = {bb.x, bb.y, bb.z, bb.w};
-#pragma unroll
-                        for (int x = 0; x < 4; ++x) {
-                            v[i + x] = __uint_as_float(r[c0 + q * kPer + i + x]) + add[x];
-                            if (p.relu) v[i + x] = v[i + x] < 0.f ? 0.f : v[i + x];   // NaN stays
-                        }
-                    }
-                    uint4 o;
-                    if constexpr (sizeof(T) == 2) {
-                        uint32_t pk[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const __nv_bfloat162 hh = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-                            pk[i] = *reinterpret_cast<const uint32_t *>(&hh);
-                        }
-                        o = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-                    } else {
-                        o = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-                    }
-                    *reinterpret_cast<uint4 *>(sb + lane * 128 + ((q ^ (lane & 7)) << 4)) = o;
-                }
-                if (p.wide) {
-                    // rows and columns behind the end are not stored
-                    fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (row0 < p.m) tma_store_2d(&tmO, smem_u32(sb), col, (int)row0);
-                        bulk_commit();
-                    }
-                    slab ^= 1;
-                } else {
-                    __syncwarp();
-                    // a row at a time, a lane to an element
-                    T *out = static_cast<T *>(p.out);
-                    for (int rr = 0; rr < 32 && row0 + rr < p.m; ++rr) {
-#pragma unroll
-                        for (int x = lane; x < kCols; x += 32)
-                            if (col + x < p.n) out[(row0 + rr) * p.out_stride + col + x] = *reinterpret_cast<const T *>(sb + rr * 128 + ((x / kPer ^ (rr & 7)) << 4) + x % kPer * sizeof(T));
-                    }
-                    __syncwarp();
-                }
-            }
+            store_half<T>(p, tmO, tmem + ((uint32_t)(w * 32) << 16) + (uint32_t)(b * 128 + half * 64), row0, n0, stg, slab, bias_s, smem_u32(acc_empty + b));
         }
         if (lane == 0) bulk_wait<0>();   // all stores of this warp have reached global memory
     }
@@ -265,6 +276,201 @@ __global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_
     tc_fence_before();
     __syncthreads();
     if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// The same product for rows that are not quantised yet and n <= 256, where all of W stays in shared memory: one kernel, so that the codes of x never go through
+// memory.  A CTA per SM walks over bands of 128 rows; warps 0-15 load x (two parts of 32 KB ahead, in registers), quantise it and write codes and scales where the tensor core
+// takes them (a ring of stages of 256 k); 16 issues; 18-25 store the accumulators, of which there are three, of 128 columns each.
+struct NarrowCfg {
+    static constexpr int kLoaders = 16, kThreads = 26 * 32;
+    static constexpr int kStages = 3;
+    static constexpr int kStageBytes = kBM * 128 + 1024;
+    static constexpr int kAccs = 3;
+    static constexpr size_t kFixed = 1024 + kStages * kStageBytes + GemmCfg::kOutBytes + 256 + 8 * 64 * 4;   // (beside W)
+    static constexpr size_t kMost = 227 * 1024;
+    static constexpr int kScaleAt = kAccs * 128;   // tensor-memory columns of the scales: x by stage, then W
+};
+static_assert(NarrowCfg::kFixed > 114 * 1024, "one CTA per multiprocessor: it takes all of the tensor memory");
+
+// Bytes of W [n x k] in shared memory: stages of 128 rows x 256 k, scale tiles.
+inline size_t narrow_w_bytes(int n, int k) { return (size_t)((n + 127) / 128) * (((size_t)k + kStageK - 1) / kStageK * 16384 + (size_t)mx_scale_tiles(k) * 512); }
+
+template <typename T>
+__global__ void __launch_bounds__(NarrowCfg::kThreads, 1) k_mx4_narrow(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmO, const GemmParams p,
+                                                                      const T *__restrict__ x, int64_t x_stride)
+{
+    using C = NarrowCfg;
+    constexpr int kS = C::kStages;
+    extern __shared__ unsigned char smem_dyn[];
+    unsigned char *base = reinterpret_cast<unsigned char *>(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
+    const int nb = p.n_tiles, stages = (p.k + kStageK - 1) / kStageK, sc_tiles = mx_scale_tiles(p.k);
+    unsigned char *smA = base, *smASc = smA + kS * kBM * 128, *smOut = smASc + kS * 1024;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smOut + GemmCfg::kOutBytes);
+    float *smBias = reinterpret_cast<float *>(smOut + GemmCfg::kOutBytes + 256);
+    unsigned char *smW = smA + (C::kFixed - 1024 + 1023) / 1024 * 1024, *smWSc = smW + (size_t)nb * stages * 16384;   // [block][stage], [block][scale tile]
+    uint64_t *full = bars, *empty = full + kS, *acc_full = empty + kS, *acc_empty = acc_full + C::kAccs, *w_full = acc_empty + C::kAccs;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(w_full + 1);
+    volatile uint32_t *abort_flag = tmem_slot + 1;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (tid == 0) {
+        for (int s = 0; s < kS; ++s) mbar_init(smem_u32(full + s), C::kLoaders), mbar_init(smem_u32(empty + s), 1);
+        for (int b = 0; b < C::kAccs; ++b) mbar_init(smem_u32(acc_full + b), 1), mbar_init(smem_u32(acc_empty + b), 8);
+        mbar_init(smem_u32(w_full), 1);
+        *abort_flag = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == C::kLoaders) tmem_alloc(smem_u32(tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    grid_dep_wait();
+    grid_dep_launch();
+
+    if (warp < C::kLoaders) {
+        // A part is kRows rows of each thread x 128 columns of the band: sixteen lanes to a row, eight elements each.
+        constexpr int kRows = sizeof(T) == 2 ? 4 : 2, kParts = 4 / kRows;
+        const int sub = tid & 15, r0 = tid >> 4;
+        int64_t band = blockIdx.x;      // of the part that is loaded next
+        int chunk = 0, part = 0;
+        auto load = [&](Raw8<T> (&v)[kRows]) {
+            const int col = chunk * 128 + sub * 8;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int64_t row = band * kBM + (part * kRows + i) * 32 + r0;
+                v[i] = Raw8<T>{};
+                if (row < p.m && col < p.k) v[i] = load_raw8<T, true>(x + row * x_stride + col);
+            }
+            if (++part == kParts) {
+                part = 0;
+                if (++chunk == sc_tiles) chunk = 0, band += gridDim.x;
+            }
+        };
+        Raw8<T> v[2][kRows];
+        load(v[0]);
+        load(v[1]);
+        uint32_t it = 0;
+        int c = 0, q = 0;   // chunk and part at work
+        bool ok = true;
+        for (int64_t at = blockIdx.x; ok && at * kBM < p.m;) {
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                if (at * kBM >= p.m) break;
+                const uint32_t s = it % kS;
+                if ((c & 1) == 0 && q == 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(empty + s), ((it / kS) & 1u) ^ 1u, abort_flag))) {
+                    ok = false;
+                    break;
+                }
+                unsigned char *codes = smA + s * kBM * 128, *scales = smASc + s * 1024 + (c & 1) * 512;
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    const int r = (q * kRows + i) * 32 + r0;
+                    uint32_t byte;
+                    const uint32_t w = mx_quantise_quad<T>(v[d][i], byte);
+                    // 16-byte pieces of a row's 128 bytes are swizzled by the row
+                    *reinterpret_cast<uint32_t *>(codes + r * 128 + ((((c & 1) * 4 + (sub >> 2)) ^ (r & 7)) << 4) + (sub & 3) * 4) = w;
+                    if ((sub & 3) == 0) scales[mx_scale_at(r, sub >> 2)] = (uint8_t)byte;
+                }
+                load(v[d]);
+                if (++q == kParts) {
+                    q = 0;
+                    const bool last = c + 1 == sc_tiles;
+                    if ((c & 1) || last) {
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(full + s));
+                        ++it;
+                    }
+                    c = last ? 0 : c + 1;
+                    if (last) at += gridDim.x;
+                }
+            }
+        }
+    } else if (warp == C::kLoaders) {
+        const uint32_t one = elect_one();
+        if (one) {
+            const uint32_t bar = smem_u32(w_full);
+            mbar_expect_tx(bar, (uint32_t)(nb * (stages * 16384 + sc_tiles * 512)));
+            for (int b = 0; b < nb; ++b) {
+                for (int j = 0; j < stages; ++j) tma_load_2d(smem_u32(smW + (b * stages + j) * 16384), &tmW, bar, j * 128, b * kBN);
+                bulk_load(smem_u32(smWSc + b * sc_tiles * 512), p.w_scales + (size_t)b * sc_tiles * 512, (uint32_t)(sc_tiles * 512), bar);
+            }
+        }
+        __syncwarp();
+        const uint64_t ad0 = umma_desc_sw128(smem_u32(smA)), bd0 = umma_desc_sw128(smem_u32(smW)), sd0 = umma_desc_plain(smem_u32(smASc), 16),
+                       wd0 = umma_desc_plain(smem_u32(smWSc), 16);
+        const uint32_t x_sc = tmem + C::kScaleAt, w_sc = x_sc + kS * 8;
+        bool ok = mbar_wait(smem_u32(w_full), 0u, abort_flag);
+        tc_fence_after();
+        if (ok)
+            for (int i = 0; i < nb * sc_tiles; ++i) tmem_copy_scales(one, w_sc + 4 * i, wd0 + (uint64_t)(i * (512 >> 4)));
+        uint32_t it = 0, acc = 0;
+        for (int64_t band = blockIdx.x; ok && band * kBM < p.m; band += gridDim.x, acc += nb) {
+            for (int j = 0; ok && j < stages; ++j, ++it) {
+                const uint32_t s = it % kS;
+                if (!mbar_wait(smem_u32(full + s), (it / kS) & 1u, abort_flag)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const int steps = min(4, (p.k - j * kStageK + 63) / 64);   // products of 64 k; codes behind the last column are zero
+                const uint64_t ad = ad0 + (uint64_t)(s * (kBM * 128 >> 4)), sd = sd0 + (uint64_t)(s * (1024 >> 4));
+                const uint32_t a_sc = x_sc + s * 8;
+                tmem_copy_scales(one, a_sc, sd);
+                if (steps > 2) tmem_copy_scales(one, a_sc + 4, sd + (uint64_t)(512 >> 4));
+                for (int b = 0; b < nb; ++b) {
+                    const uint32_t n_acc = acc + b, slot = n_acc % C::kAccs;
+                    if (j == 0 && n_acc >= C::kAccs && !mbar_wait(smem_u32(acc_empty + slot), ((n_acc / C::kAccs) & 1u) ^ 1u, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint64_t bd = bd0 + (uint64_t)((b * stages + j) * (16384 >> 4));
+                    const uint32_t b_sc = w_sc + 4 * (uint32_t)(b * sc_tiles + 2 * j);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (q >= steps) break;
+                        umma_mxf4(one, tmem + slot * 128, ad + 2 * q, bd + 2 * q, umma_idesc_mxf4(kBM, kBN, (q & 1) * 2), a_sc + 4 * (q >> 1), b_sc + 4 * (q >> 1), j > 0 || q > 0);
+                    }
+                    if (j + 1 == stages) umma_commit_if(one, smem_u32(acc_full + slot));
+                }
+                umma_commit_if(one, smem_u32(empty + s));
+            }
+        }
+    } else if (warp >= C::kLoaders + 2) {
+        const int e = warp - C::kLoaders - 2, w = warp & 3, half = e >> 2;
+        unsigned char *stg = smOut + e * 2 * 4096;
+        float *bias_s = smBias + e * 64;
+        int slab = 0;
+        uint32_t acc = 0;
+        bool ok = true;
+        for (int64_t band = blockIdx.x; ok && band * kBM < p.m; band += gridDim.x) {
+            for (int b = 0; b < nb; ++b, ++acc) {
+                const uint32_t slot = acc % C::kAccs;
+                const int n0 = b * kBN + half * 64;
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 64; i += 32) bias_s[i + lane] = p.bias && n0 + i + lane < p.n ? __ldg(p.bias + n0 + i + lane) : 0.f;
+                __syncwarp();
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(acc_full + slot), (acc / C::kAccs) & 1u, abort_flag))) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                store_half<T>(p, tmO, tmem + ((uint32_t)(w * 32) << 16) + slot * 128u + (uint32_t)(half * 64), band * kBM + w * 32, n0, stg, slab, bias_s, smem_u32(acc_empty + slot));
+            }
+        }
+        if (lane == 0) bulk_wait<0>();   // all stores of this warp have reached global memory
+    }
+
+    if (*abort_flag) {
+        if (tid == 0 && p.status) atomicOr(p.status, AIF_STATUS_TIMEOUT);
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000ll) __nanosleep(1000);   // copies in flight land before the memory is given up
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == C::kLoaders) tmem_dealloc(tmem, 512);
 }
 
 // Codes as a matrix of bytes [rows x cols / 2], boxes of 128 bytes x box_rows, 128-byte swizzle; columns and rows behind the end read as zero.
@@ -282,30 +488,57 @@ cudaError_t encode_codes(CUtensorMap *m, const uint8_t *codes, int64_t rows, int
 }
 
 template <typename T>
+cudaError_t encode_out(CUtensorMap *m, const GemmParams &p)
+{
+    // the output as it is stored: 128-byte pieces of 32 rows
+    if (!p.wide) return cudaSuccess;
+    EncodeFn enc = encode_fn();
+    if (!enc) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {(cuuint64_t)p.n, (cuuint64_t)p.m};
+    const cuuint64_t strides[1] = {(cuuint64_t)(p.out_stride * sizeof(T))};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / sizeof(T)), 32};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = enc(m, sizeof(T) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, p.out, dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <typename T>
 cudaError_t run_gemm(GemmParams p, const uint8_t *a_codes, const uint8_t *w_codes, cudaStream_t st)
 {
     using C = GemmCfg;
     CUtensorMap ta, tw, to{};
     cudaError_t e = encode_codes(&ta, a_codes, p.m, p.k, kBM);
     if (e == cudaSuccess) e = encode_codes(&tw, w_codes, p.n, p.k, kBN);
-    if (e == cudaSuccess && p.wide) {
-        // the output as it is stored: 128-byte pieces of 32 rows
-        const cuuint64_t dims[2] = {(cuuint64_t)p.n, (cuuint64_t)p.m};
-        const cuuint64_t strides[1] = {(cuuint64_t)(p.out_stride * sizeof(T))};
-        const cuuint32_t box[2] = {(cuuint32_t)(128 / sizeof(T)), 32};
-        const cuuint32_t estr[2] = {1, 1};
-        const CUresult r = encode_fn()(&to, sizeof(T) == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, p.out, dims, strides, box, estr,
-                                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-        if (r != CUDA_SUCCESS) e = cudaErrorInvalidValue;
-    }
+    if (e == cudaSuccess) e = encode_out<T>(&to, p);
     if (e == cudaSuccess) e = allow_smem<k_mx4_gemm<T>>(C::kSmem);
     if (e != cudaSuccess) return e;
-    p.n_tiles = (p.n + kBN - 1) / kBN;
     p.tiles = (p.m + kBM - 1) / kBM * p.n_tiles;
     const unsigned grid = (unsigned)(p.tiles < 148 ? p.tiles : 148);
     e = launch_pdl(k_mx4_gemm<T>, dim3(grid), dim3(C::kThreads), C::kSmem, st, ta, tw, to, p);
     count_launch();
     return e;
+}
+template <typename T>
+cudaError_t run_narrow(const GemmParams &p, const void *x, int64_t x_stride, const uint8_t *w_codes, cudaStream_t st)
+{
+    using C = NarrowCfg;
+    CUtensorMap tw, to{};
+    cudaError_t e = encode_codes(&tw, w_codes, p.n, p.k, kBN);
+    if (e == cudaSuccess) e = encode_out<T>(&to, p);
+    const size_t smem = (C::kFixed + 1023) / 1024 * 1024 + narrow_w_bytes(p.n, p.k);
+    if (e == cudaSuccess) e = allow_smem<k_mx4_narrow<T>>(C::kMost);
+    if (e != cudaSuccess) return e;
+    const int64_t bands = (p.m + kBM - 1) / kBM;
+    e = launch_pdl(k_mx4_narrow<T>, dim3((unsigned)(bands < 148 ? bands : 148)), dim3(C::kThreads), smem, st, tw, to, p, static_cast<const T *>(x), x_stride);
+    count_launch();
+    return e;
+}
+// W fits beside the rest, and rows begin on 16 bytes.
+bool narrow_fits(const aif_mx4_product &q, int el)
+{
+    return q.n <= 256 && (NarrowCfg::kFixed + 1023) / 1024 * 1024 + narrow_w_bytes(q.n, q.k) <= NarrowCfg::kMost && (reinterpret_cast<uintptr_t>(q.x) & 15) == 0 &&
+           (q.x_stride * el) % 16 == 0;
 }
 
 }  // namespace
@@ -334,23 +567,30 @@ int aif_mx4_linear(const aif_mx4_product *q, aif_stream stream)
     if (!aligned(q->w_codes) || !aligned(q->w_scales) || !q->out || reinterpret_cast<uintptr_t>(q->out) % el != 0) return AIF_ERR_ARG;
     if (q->bias && reinterpret_cast<uintptr_t>(q->bias) % 4 != 0) return AIF_ERR_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-    const uint8_t *codes = q->x_codes, *scales = q->x_scales;
+    GemmParams p{};
+    p.m = q->m, p.n = q->n, p.k = q->k, p.a_scales = q->x_scales, p.w_scales = q->w_scales, p.bias = q->bias, p.relu = q->relu;
+    p.out = q->out, p.out_stride = q->out_stride, p.status = q->status, p.n_tiles = (q->n + kBN - 1) / kBN;
+    // (a tile store cuts a row off at 16 bytes, not at an element)
+    p.wide = (reinterpret_cast<uintptr_t>(q->out) & 15) == 0 && (q->out_stride * el) % 16 == 0 && ((int64_t)q->n * el) % 16 == 0;
+    const uint8_t *codes = q->x_codes;
     cudaError_t e = cudaSuccess;
+    bool narrow = false;
     if (q->x) {
         if (q->x_stride < q->k) return AIF_ERR_SHAPE;
         if (reinterpret_cast<uintptr_t>(q->x) % el != 0 || !aligned(q->workspace) || q->workspace_bytes < aif_mx4_workspace_bytes(q->m, q->k)) return AIF_ERR_ARG;
-        uint8_t *ws = static_cast<uint8_t *>(q->workspace);
-        codes = ws, scales = ws + (q->m * (q->k / 2) + 255) / 256 * 256;
-        e = launch_mx4_quantize(q->x, q->dtype, q->m, q->k, q->x_stride, ws, const_cast<uint8_t *>(scales), st);
-    } else if (!aligned(codes) || !aligned(scales)) {
+        narrow = narrow_fits(*q, el);
+        if (!narrow) {
+            uint8_t *ws = static_cast<uint8_t *>(q->workspace), *scales = ws + (q->m * (q->k / 2) + 255) / 256 * 256;
+            codes = ws, p.a_scales = scales;
+            e = launch_mx4_quantize(q->x, q->dtype, q->m, q->k, q->x_stride, ws, scales, st);
+        }
+    } else if (!aligned(codes) || !aligned(p.a_scales)) {
         return AIF_ERR_ARG;
     }
-    GemmParams p{};
-    p.m = q->m, p.n = q->n, p.k = q->k, p.a_scales = scales, p.w_scales = q->w_scales, p.bias = q->bias, p.relu = q->relu;
-    p.out = q->out, p.out_stride = q->out_stride, p.status = q->status;
-    // (a tile store cuts a row off at 16 bytes, not at an element)
-    p.wide = (reinterpret_cast<uintptr_t>(q->out) & 15) == 0 && (q->out_stride * el) % 16 == 0 && ((int64_t)q->n * el) % 16 == 0;
-    if (e == cudaSuccess) e = q->dtype == AIF_BF16 ? run_gemm<__nv_bfloat16>(p, codes, q->w_codes, st) : run_gemm<float>(p, codes, q->w_codes, st);
+    if (narrow)
+        e = q->dtype == AIF_BF16 ? run_narrow<__nv_bfloat16>(p, q->x, q->x_stride, q->w_codes, st) : run_narrow<float>(p, q->x, q->x_stride, q->w_codes, st);
+    else if (e == cudaSuccess)
+        e = q->dtype == AIF_BF16 ? run_gemm<__nv_bfloat16>(p, codes, q->w_codes, st) : run_gemm<float>(p, codes, q->w_codes, st);
     if (e == cudaSuccess) return AIF_OK;
     char text[256];
     snprintf(text, sizeof(text), "aif_mx4_linear: %s", cudaGetErrorString(e));
