@@ -602,15 +602,15 @@ __global__ void __launch_bounds__(kRowThreads) k_append(const AppendParams p)
             }
             __syncthreads();
         }
+        uint32_t w[4], byte[4];
+        mx_quantise_quad<T>(v, w, byte);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            uint32_t byte;
-            const uint32_t w = mx_quantise_quad<T>(v[u], byte);
             if (i0 + u * kRowThreads + tid >= items || place[row[u]] < 0) continue;
             const int head = (int)p.per_head.div((uint32_t)part[u]), sub = part[u] - head * (int)p.per_head.by;
             const size_t r = (size_t)place[row[u]] + ((size_t)head << c.page_shift);
-            reinterpret_cast<uint32_t *>(c.codes[which] + r * (c.d / 2))[sub] = w;
-            if ((sub & 3) == 0) c.scales[which][r * (c.d / 32) + (sub >> 2)] = (uint8_t)byte;
+            reinterpret_cast<uint32_t *>(c.codes[which] + r * (c.d / 2))[sub] = w[u];
+            if ((sub & 3) == 0) c.scales[which][r * (c.d / 32) + (sub >> 2)] = (uint8_t)byte[u];
         }
     }
 }

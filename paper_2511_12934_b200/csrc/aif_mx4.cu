@@ -2,6 +2,7 @@
 //
 // Both are one pass over the data, bound by HBM.  A CTA takes 128 rows x 128 columns, the region of one 512-byte tile of scale
 // bytes, so that the tile leaves in one coalesced store; sixteen lanes read 256 (bf16) consecutive bytes of a row, four of them share a block.
+// 524288 x 512 in bf16: 120 us, 5.7 TB/s.
 #include <climits>
 #include <cstdio>
 
@@ -35,15 +36,15 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const T *__restrict__ x, i
             v[i] = Raw8<T>{};
             if (row < rows && col < cols) v[i] = load_raw8<T, ALIGNED>(x + row * stride + col);
         }
+        uint32_t w[4], byte[4];
+        mx_quantise_quad<T>(v, w, byte);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = (i0 + i) * 16 + (tid >> 4);
             const int64_t row = band * kTile + r;
             const bool in = row < rows && col < cols;   // the four lanes of a block agree: cols is a multiple of 32
-            uint32_t byte;
-            const uint32_t w = mx_quantise_quad<T>(v[i], byte);
-            if (in) *reinterpret_cast<uint32_t *>(codes + row * (cols / 2) + col / 2) = w;
-            if ((sub & 3) == 0) tile[mx_scale_at(r, sub >> 2)] = (uint8_t)(in ? byte : 0u);   // padding: 2^-127, which times a zero code is nothing
+            if (in) *reinterpret_cast<uint32_t *>(codes + row * (cols / 2) + col / 2) = w[i];
+            if ((sub & 3) == 0) tile[mx_scale_at(r, sub >> 2)] = (uint8_t)(in ? byte[i] : 0u);   // padding: 2^-127, which times a zero code is nothing
         }
     }
     // The product that may follow takes its place beside the last CTAs: 37.1 us against 38.4 (10000 x 2816 by 1024, with the product); in

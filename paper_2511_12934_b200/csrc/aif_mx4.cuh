@@ -122,39 +122,73 @@ __device__ __forceinline__ void store8(T *p, const float (&v)[8])
     }
 }
 
-// Larger of two pairs of bf16 magnitudes; NaN is the largest.
-__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b)
+// Larger of two pairs of bf16 magnitudes, NaN is the largest; signs mean nothing.
+__device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t a, uint32_t b)
 {
     uint32_t o;
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
     return o;
 }
-// Four neighbouring lanes (4 i .. 4 i + 3, converged) quantise the 32 elements of one block, eight each: the lane's codes, and the block's scale byte.
-template <typename T>
-__device__ __forceinline__ uint32_t mx_quantise_quad(const Raw8<T> &x, uint32_t &byte)
+__device__ __forceinline__ float max_abs_f32(float a, float b)
 {
-    uint32_t field;   // exponent field of the largest magnitude
-    if constexpr (sizeof(T) == 2) {
-        uint32_t m = max_bf16x2(max_bf16x2(x.w[0] & 0x7fff7fffu, x.w[1] & 0x7fff7fffu), max_bf16x2(x.w[2] & 0x7fff7fffu, x.w[3] & 0x7fff7fffu));
-        m = max_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 1));
-        m = max_bf16x2(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        field = max((m & 0xffffu) >> 7, m >> 23);
-    } else {
-        uint32_t top = 0;
+    float o;
+    asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(o) : "f"(a), "f"(b));
+    return o;
+}
+// Two bf16 values times a power of two (its upper half), exactly, as fp32; -0 stays.
+__device__ __forceinline__ void scale_bf16x2(uint32_t x, uint32_t power, float &lo, float &hi)
+{
+    asm("{\n"
+        ".reg .b16 l, h, none, p;\n"
+        "mov.b32 {l, h}, %2;\n"
+        "mov.b32 {none, p}, %3;\n"
+        "fma.rn.f32.bf16 %0, l, p, %4;\n"
+        "fma.rn.f32.bf16 %1, h, p, %4;\n"
+        "}\n"
+        : "=f"(lo), "=f"(hi)
+        : "r"(x), "r"(power), "f"(-0.f));
+}
+// Four neighbouring lanes (4 i .. 4 i + 3, converged) quantise the 32 elements of each of N blocks, eight each: the lane's codes, and the blocks' scale bytes.  Blocks go in
+// pairs: their largest magnitudes (the upper 16 bits say all that is needed of them) share a register on their way through the lanes.
+template <typename T, int N>
+__device__ __forceinline__ void mx_quantise_quad(const Raw8<T> (&x)[N], uint32_t (&w)[N], uint32_t (&byte)[N])
+{
+    static_assert(N % 2 == 0, "blocks go in pairs");
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, x.w[i] & 0x7fffffffu);   // as integers: NaN stays the largest
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        field = top >> 23;
+    for (int n = 0; n < N; n += 2) {
+        uint32_t top;   // of block n in the lower half
+        if constexpr (sizeof(T) == 2) {
+            uint32_t m[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) m[i] = max_abs_bf16x2(max_abs_bf16x2(x[n + i].w[0], x[n + i].w[1]), max_abs_bf16x2(x[n + i].w[2], x[n + i].w[3]));
+            top = max_abs_bf16x2(__byte_perm(m[0], m[1], 0x5410), __byte_perm(m[0], m[1], 0x7632));
+        } else {
+            float m[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                m[i] = __uint_as_float(x[n + i].w[0]);
+#pragma unroll
+                for (int e = 1; e < 8; ++e) m[i] = max_abs_f32(m[i], __uint_as_float(x[n + i].w[e]));
+            }
+            top = __byte_perm(__float_as_uint(m[0]), __float_as_uint(m[1]), 0x7632);
+        }
+        top = max_abs_bf16x2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max_abs_bf16x2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t b = mx_scale_byte((top >> (i ? 23 : 7)) & 0xffu), inv = __float_as_uint(mx_inverse_scale(b));
+            float v[8];
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) scale_bf16x2(x[n + i].w[e], inv, v[2 * e], v[2 * e + 1]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(x[n + i].w[e]) * __uint_as_float(inv);
+            }
+            const uint32_t codes = mx_encode8(v);
+            w[n + i] = b == kMxNan ? 0u : codes, byte[n + i] = b;
+        }
     }
-    byte = mx_scale_byte(field);
-    const float inv = mx_inverse_scale(byte);
-    float v[8];
-    widen8<T>(x, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= inv;
-    const uint32_t w = mx_encode8(v);
-    return byte == kMxNan ? 0u : w;
 }
 // The values of eight codes of a block with this scale.
 __device__ __forceinline__ void mx_values8(uint32_t codes, float scale, float (&v)[8])

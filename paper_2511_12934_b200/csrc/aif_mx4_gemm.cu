@@ -7,6 +7,7 @@
 // 1 copies a stage's scales to tensor memory and issues its four products of 64 k; 4-11 take a finished accumulator out of tensor memory while the
 // next tile is at work (two accumulators) and store it through shared memory with asynchronous tile stores.
 // The scale copies go to tensor-memory columns of their own per stage: a stage is only refilled once its products have completed.
+// 4096 x 4096 x 4096: 37.6 us, 3.7 PFLOP/s; 10000 x 2816 by 1024: 20.3 us (bound: its tail, 632 tiles on 148 multiprocessors), 34.9 us with the quantisation of x; 7 rows: 5.5 us.
 #include <climits>
 #include <cstdio>
 
@@ -77,10 +78,22 @@ struct GemmParams {
     int64_t out_stride;
     int32_t wide;        // rows of `out` begin and end on 16-byte boundaries: tile stores
     int32_t n_tiles;     // column tiles
-    int64_t tiles;
+    int64_t tiles;       // all (of the kernel that quantises too: bands of rows)
     uint32_t *status;
 };
 
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t o;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
+    return o;
+}
+__device__ __forceinline__ float max_nan_f32(float a, float b)
+{
+    float o;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(o) : "f"(a), "f"(b));
+    return o;
+}
 // 32 rows x 64 columns of an accumulator, by one warp: from tensor memory through shared memory (two slabs of 4 KB) to `out`, in pieces of 128 bytes of a row, swizzled
 // so that the lanes (one row each) stay on different banks and a tile store takes them in the same form.  `freed` is told once the accumulator has been read.
 template <typename T>
@@ -90,6 +103,7 @@ __device__ __forceinline__ void store_half(const GemmParams &p, const CUtensorMa
     constexpr int kCols = 128 / (int)sizeof(T);   // columns of a piece
     constexpr int kPer = 16 / (int)sizeof(T);     // elements of 16 bytes
     const int lane = threadIdx.x & 31;
+    const uint32_t least = p.relu ? 0u : sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;   // the larger of this and the value, where NaN stays
 #pragma unroll
     for (int c0 = 0; c0 < 64; c0 += 32) {
         uint32_t r[32];
@@ -114,10 +128,7 @@ __device__ __forceinline__ void store_half(const GemmParams &p, const CUtensorMa
                 const float4 bb = *reinterpret_cast<const float4 *>(bias_s + c0 + q * kPer + i);
                 const float add[4] = {bb.x, bb.y, bb.z, bb.w};
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    v[i + x] = __uint_as_float(r[q * kPer + i + x]) + add[x];
-                    if (p.relu) v[i + x] = v[i + x] < 0.f ? 0.f : v[i + x];   // NaN stays
-                }
+                for (int x = 0; x < 4; ++x) v[i + x] = __uint_as_float(r[q * kPer + i + x]) + add[x];
             }
             uint4 o;
             if constexpr (sizeof(T) == 2) {
@@ -125,10 +136,12 @@ __device__ __forceinline__ void store_half(const GemmParams &p, const CUtensorMa
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const __nv_bfloat162 hh = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-                    pk[i] = *reinterpret_cast<const uint32_t *>(&hh);
+                    pk[i] = max_nan_bf16x2(*reinterpret_cast<const uint32_t *>(&hh), least);
                 }
                 o = make_uint4(pk[0], pk[1], pk[2], pk[3]);
             } else {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) v[i] = max_nan_f32(v[i], __uint_as_float(least));
                 o = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
             }
             *reinterpret_cast<uint4 *>(sb + lane * 128 + (((q + (c0 - first) / kPer) ^ (lane & 7)) << 4)) = o;
@@ -280,17 +293,19 @@ __global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_
 
 // The same product for rows that are not quantised yet and n <= 256, where all of W stays in shared memory: one kernel, so that the codes of x never go through
 // memory.  A CTA per SM walks over bands of 128 rows; warps 0-15 load x (two parts of 32 KB ahead, in registers), quantise it and write codes and scales where the tensor core
-// takes them (a ring of stages of 256 k); 16 issues; 18-25 store the accumulators, of which there are three, of 128 columns each.
+// takes them (a ring of stages of 256 k); 16 issues; 17-20 store the accumulators, of which there are three, of 128 columns each.  Bound: HBM.  524288 x 512 by 256 in bf16:
+// 137 us, 5.9 TB/s (quantising first: 192 us; in chunks that stay in L2, 215 us at best, their launches cost more than that saves); 524288 x 256 by 128: bf16 68 us, fp32 128 us.
 struct NarrowCfg {
-    static constexpr int kLoaders = 16, kThreads = 26 * 32;
+    static constexpr int kLoaders = 16, kThreads = 21 * 32;
     static constexpr int kStages = 3;
     static constexpr int kStageBytes = kBM * 128 + 1024;
     static constexpr int kAccs = 3;
-    static constexpr size_t kFixed = 1024 + kStages * kStageBytes + GemmCfg::kOutBytes + 256 + 8 * 64 * 4;   // (beside W)
+    static constexpr int kOutBytes = 4 * 2 * 4096;
+    static constexpr size_t kFixed = 1024 + kStages * kStageBytes + kOutBytes + 256 + 4 * 128 * 4;   // (beside W)
+    static constexpr size_t kLeast = 116 * 1024;   // one CTA per multiprocessor: it takes all of the tensor memory
     static constexpr size_t kMost = 227 * 1024;
     static constexpr int kScaleAt = kAccs * 128;   // tensor-memory columns of the scales: x by stage, then W
 };
-static_assert(NarrowCfg::kFixed > 114 * 1024, "one CTA per multiprocessor: it takes all of the tensor memory");
 
 // Bytes of W [n x k] in shared memory: stages of 128 rows x 256 k, scale tiles.
 inline size_t narrow_w_bytes(int n, int k) { return (size_t)((n + 127) / 128) * (((size_t)k + kStageK - 1) / kStageK * 16384 + (size_t)mx_scale_tiles(k) * 512); }
@@ -305,8 +320,8 @@ __global__ void __launch_bounds__(NarrowCfg::kThreads, 1) k_mx4_narrow(const __g
     unsigned char *base = reinterpret_cast<unsigned char *>(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
     const int nb = p.n_tiles, stages = (p.k + kStageK - 1) / kStageK, sc_tiles = mx_scale_tiles(p.k);
     unsigned char *smA = base, *smASc = smA + kS * kBM * 128, *smOut = smASc + kS * 1024;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smOut + GemmCfg::kOutBytes);
-    float *smBias = reinterpret_cast<float *>(smOut + GemmCfg::kOutBytes + 256);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smOut + C::kOutBytes);
+    float *smBias = reinterpret_cast<float *>(smOut + C::kOutBytes + 256);
     unsigned char *smW = smA + (C::kFixed - 1024 + 1023) / 1024 * 1024, *smWSc = smW + (size_t)nb * stages * 16384;   // [block][stage], [block][scale tile]
     uint64_t *full = bars, *empty = full + kS, *acc_full = empty + kS, *acc_empty = acc_full + C::kAccs, *w_full = acc_empty + C::kAccs;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(w_full + 1);
@@ -331,47 +346,50 @@ __global__ void __launch_bounds__(NarrowCfg::kThreads, 1) k_mx4_narrow(const __g
         // A part is kRows rows of each thread x 128 columns of the band: sixteen lanes to a row, eight elements each.
         constexpr int kRows = sizeof(T) == 2 ? 4 : 2, kParts = 4 / kRows;
         const int sub = tid & 15, r0 = tid >> 4;
-        int64_t band = blockIdx.x;      // of the part that is loaded next
-        int chunk = 0, part = 0;
+        const int64_t row_step = 32 * x_stride * (int64_t)sizeof(T), band_step = (int64_t)gridDim.x * kBM * x_stride * (int64_t)sizeof(T);   // bytes
+        // of the part that is loaded next: this thread's first row and column in it, and how many rows there are from there on
+        const char *src = reinterpret_cast<const char *>(x + ((int64_t)blockIdx.x * kBM + r0) * x_stride + sub * 8);
+        int have = (int)p.m - (int)blockIdx.x * kBM - r0, col = sub * 8, part = 0;
         auto load = [&](Raw8<T> (&v)[kRows]) {
-            const int col = chunk * 128 + sub * 8;
+            const int rows = col < p.k ? have : 0;
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
-                const int64_t row = band * kBM + (part * kRows + i) * 32 + r0;
                 v[i] = Raw8<T>{};
-                if (row < p.m && col < p.k) v[i] = load_raw8<T, true>(x + row * x_stride + col);
+                if (i * 32 < rows) v[i] = load_raw8<T, true>(reinterpret_cast<const T *>(src));
+                src += row_step;
             }
+            have -= kRows * 32;
             if (++part == kParts) {
-                part = 0;
-                if (++chunk == sc_tiles) chunk = 0, band += gridDim.x;
+                part = 0, have += kBM, col += 128, src += 128 * (int)sizeof(T) - 4 * row_step;
+                if (col >= sc_tiles * 128) src += band_step - (col - sub * 8) * (int)sizeof(T), have -= (int)gridDim.x * kBM, col = sub * 8;
             }
         };
         Raw8<T> v[2][kRows];
         load(v[0]);
         load(v[1]);
-        uint32_t it = 0;
-        int c = 0, q = 0;   // chunk and part at work
-        bool ok = true;
-        for (int64_t at = blockIdx.x; ok && at * kBM < p.m;) {
+        // 16-byte pieces of a row's 128 bytes of codes are swizzled by the row (a part's rows are 32 apart): both halves of a stage
+        const uint32_t codes_at = smem_u32(smA) + r0 * 128 + (((sub >> 2) ^ (r0 & 7)) << 4) + (sub & 3) * 4, scales_at = smem_u32(smASc) + mx_scale_at(r0, sub >> 2);
+        uint32_t s = 0, phase = 1;   // stage, and the parity of the wait for it
+        int c = 0, q = 0;            // chunk and part at work
+        const int mine = (int)((p.tiles + gridDim.x - 1 - blockIdx.x) / gridDim.x);   // bands
+        for (int parts = mine * sc_tiles * kParts; parts > 0;) {
 #pragma unroll
             for (int d = 0; d < 2; ++d) {
-                if (at * kBM >= p.m) break;
-                const uint32_t s = it % kS;
-                if ((c & 1) == 0 && q == 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(empty + s), ((it / kS) & 1u) ^ 1u, abort_flag))) {
-                    ok = false;
+                if (parts <= 0) break;
+                if ((c & 1) == 0 && q == 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(empty + s), phase, abort_flag))) {
+                    parts = 0;
                     break;
                 }
-                unsigned char *codes = smA + s * kBM * 128, *scales = smASc + s * 1024 + (c & 1) * 512;
+                --parts;
+                uint32_t w[kRows], byte[kRows];
+                mx_quantise_quad<T>(v[d], w, byte);
+                load(v[d]);
+                const uint32_t to = (codes_at ^ (uint32_t)((c & 1) << 6)) + s * (kBM * 128) + q * (kRows * 32 * 128), sc_to = scales_at + s * 1024 + (c & 1) * 512 + q * (kRows * 4);
 #pragma unroll
                 for (int i = 0; i < kRows; ++i) {
-                    const int r = (q * kRows + i) * 32 + r0;
-                    uint32_t byte;
-                    const uint32_t w = mx_quantise_quad<T>(v[d][i], byte);
-                    // 16-byte pieces of a row's 128 bytes are swizzled by the row
-                    *reinterpret_cast<uint32_t *>(codes + r * 128 + ((((c & 1) * 4 + (sub >> 2)) ^ (r & 7)) << 4) + (sub & 3) * 4) = w;
-                    if ((sub & 3) == 0) scales[mx_scale_at(r, sub >> 2)] = (uint8_t)byte;
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + i * (32 * 128)), "r"(w[i]) : "memory");
+                    if ((sub & 3) == 0) asm volatile("st.shared.b8 [%0], %1;" ::"r"(sc_to + i * 4), "r"(byte[i]) : "memory");
                 }
-                load(v[d]);
                 if (++q == kParts) {
                     q = 0;
                     const bool last = c + 1 == sc_tiles;
@@ -379,10 +397,9 @@ __global__ void __launch_bounds__(NarrowCfg::kThreads, 1) k_mx4_narrow(const __g
                         fence_proxy_async();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(smem_u32(full + s));
-                        ++it;
+                        if (++s == kS) s = 0, phase ^= 1u;
                     }
                     c = last ? 0 : c + 1;
-                    if (last) at += gridDim.x;
                 }
             }
         }
@@ -437,27 +454,31 @@ __global__ void __launch_bounds__(NarrowCfg::kThreads, 1) k_mx4_narrow(const __g
                 umma_commit_if(one, smem_u32(empty + s));
             }
         }
-    } else if (warp >= C::kLoaders + 2) {
-        const int e = warp - C::kLoaders - 2, w = warp & 3, half = e >> 2;
+    } else {
+        // a warp to a quarter of the rows
+        const int e = warp - C::kLoaders - 1, w = warp & 3;
         unsigned char *stg = smOut + e * 2 * 4096;
-        float *bias_s = smBias + e * 64;
+        float *bias_s = smBias + e * 128;
         int slab = 0;
         uint32_t acc = 0;
         bool ok = true;
         for (int64_t band = blockIdx.x; ok && band * kBM < p.m; band += gridDim.x) {
             for (int b = 0; b < nb; ++b, ++acc) {
                 const uint32_t slot = acc % C::kAccs;
-                const int n0 = b * kBN + half * 64;
+                const int n0 = b * kBN;
                 __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 64; i += 32) bias_s[i + lane] = p.bias && n0 + i + lane < p.n ? __ldg(p.bias + n0 + i + lane) : 0.f;
+                for (int i = 0; i < 128; i += 32) bias_s[i + lane] = p.bias && n0 + i + lane < p.n ? __ldg(p.bias + n0 + i + lane) : 0.f;
                 __syncwarp();
                 if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(acc_full + slot), (acc / C::kAccs) & 1u, abort_flag))) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                store_half<T>(p, tmO, tmem + ((uint32_t)(w * 32) << 16) + slot * 128u + (uint32_t)(half * 64), band * kBM + w * 32, n0, stg, slab, bias_s, smem_u32(acc_empty + slot));
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half)
+                    store_half<T>(p, tmO, tmem + ((uint32_t)(w * 32) << 16) + slot * 128u + (uint32_t)(half * 64), band * kBM + w * 32, n0 + half * 64, stg, slab, bias_s + half * 64,
+                                  smem_u32(acc_empty + slot));
             }
         }
         if (lane == 0) bulk_wait<0>();   // all stores of this warp have reached global memory
@@ -520,25 +541,29 @@ cudaError_t run_gemm(GemmParams p, const uint8_t *a_codes, const uint8_t *w_code
     return e;
 }
 template <typename T>
-cudaError_t run_narrow(const GemmParams &p, const void *x, int64_t x_stride, const uint8_t *w_codes, cudaStream_t st)
+cudaError_t run_narrow(GemmParams p, const void *x, int64_t x_stride, const uint8_t *w_codes, cudaStream_t st)
 {
     using C = NarrowCfg;
     CUtensorMap tw, to{};
     cudaError_t e = encode_codes(&tw, w_codes, p.n, p.k, kBN);
     if (e == cudaSuccess) e = encode_out<T>(&to, p);
-    const size_t smem = (C::kFixed + 1023) / 1024 * 1024 + narrow_w_bytes(p.n, p.k);
+    const size_t need = (C::kFixed + 1023) / 1024 * 1024 + narrow_w_bytes(p.n, p.k), smem = need < C::kLeast ? C::kLeast : need;
     if (e == cudaSuccess) e = allow_smem<k_mx4_narrow<T>>(C::kMost);
     if (e != cudaSuccess) return e;
-    const int64_t bands = (p.m + kBM - 1) / kBM;
-    e = launch_pdl(k_mx4_narrow<T>, dim3((unsigned)(bands < 148 ? bands : 148)), dim3(C::kThreads), smem, st, tw, to, p, static_cast<const T *>(x), x_stride);
+    p.tiles = (p.m + kBM - 1) / kBM;
+    e = launch_pdl(k_mx4_narrow<T>, dim3((unsigned)(p.tiles < 148 ? p.tiles : 148)), dim3(C::kThreads), smem, st, tw, to, p, static_cast<const T *>(x), x_stride);
     count_launch();
     return e;
 }
-// W fits beside the rest, and rows begin on 16 bytes.
-bool narrow_fits(const aif_mx4_product &q, int el)
+// The kernel that quantises the rows itself: rows begin on 16 bytes, n <= 256 and W fits beside the rest.  It reads x once and writes nothing but `out`; what speaks against
+// it is the time of one band, which grows with k.  So: short rows (k of 256 in bf16 and 1000 rows: 4.9 us against 6.2 of the two kernels), or two bands per multiprocessor and
+// more (k 512, n 256, bf16: 37888 rows 13.6 us against 15.6, but 20000 rows, two bands for a few, 13.0 against 12.0 and 1000 rows 8.0 against 6.6; 300000 rows 80 against 115).
+// fp32 also needs the L1 that a large W takes (300000 x 1024 in fp32: n 128 224 us against 250, n 256 311 against 288; in bf16 n 256 146 against 202).
+bool use_narrow(const aif_mx4_product &q, int el)
 {
-    return q.n <= 256 && (NarrowCfg::kFixed + 1023) / 1024 * 1024 + narrow_w_bytes(q.n, q.k) <= NarrowCfg::kMost && (reinterpret_cast<uintptr_t>(q.x) & 15) == 0 &&
-           (q.x_stride * el) % 16 == 0;
+    const size_t w = narrow_w_bytes(q.n, q.k);
+    const bool can = q.n <= 256 && (NarrowCfg::kFixed + 1023) / 1024 * 1024 + w <= NarrowCfg::kMost && (reinterpret_cast<uintptr_t>(q.x) & 15) == 0 && (q.x_stride * el) % 16 == 0;
+    return can && (el == 2 || w <= 76 * 1024) && (q.k * el <= 512 || q.m > 2 * 147 * kBM);
 }
 
 }  // namespace
@@ -578,7 +603,7 @@ int aif_mx4_linear(const aif_mx4_product *q, aif_stream stream)
     if (q->x) {
         if (q->x_stride < q->k) return AIF_ERR_SHAPE;
         if (reinterpret_cast<uintptr_t>(q->x) % el != 0 || !aligned(q->workspace) || q->workspace_bytes < aif_mx4_workspace_bytes(q->m, q->k)) return AIF_ERR_ARG;
-        narrow = narrow_fits(*q, el);
+        narrow = use_narrow(*q, el);
         if (!narrow) {
             uint8_t *ws = static_cast<uint8_t *>(q->workspace), *scales = ws + (q->m * (q->k / 2) + 255) / 256 * 256;
             codes = ws, p.a_scales = scales;

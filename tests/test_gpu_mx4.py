@@ -109,6 +109,23 @@ def test_linear(m, k, n, dtype, relu, with_bias):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m, k, n", [(1, 32, 1), (300, 128, 256), (1000, 96, 33), (40000, 160, 129), (37888, 512, 256), (40001, 1024, 128), (70000, 64, 8), (38000, 1088, 200), (45000, 288, 72)])
+def test_rows_quantised_within_the_product(m, k, n, dtype):
+    """Rows as they are and rows quantised before give the same bits, whichever kernels do it; another product on the stream right behind."""
+    x = (torch.randn(m, k, device="cuda") * 0.1).to(dtype)
+    x[m // 2, 5] = float("inf")
+    w, b = B.mx4_quantize(torch.randn(n, k, device="cuda")), torch.randn(n, device="cuda")
+    first, second = (torch.full((m, n), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.mx4_linear(x, w, first, bias=b, status=status)
+    B.mx4_linear(x, w, second, bias=b, status=status)
+    want = B.mx4_linear(B.mx4_quantize(x), w, torch.empty_like(first), bias=b, status=status)
+    rest = torch.arange(m, device="cuda") != m // 2
+    assert torch.equal(first[rest], want[rest]) and torch.equal(second[rest], want[rest])
+    assert torch.isnan(first[m // 2]).all() and torch.isnan(want[m // 2]).all() and status.item() == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n, pad, shift", [(40, 24, 0), (40, 3, 0), (33, 31, 0), (64, 8, 1), (130, 62, 8)])
 def test_linear_output_strides(dtype, n, pad, shift):
     m, k = 150, 64
