@@ -518,19 +518,8 @@ __device__ __forceinline__ int entry_of(const int64_t *offsets, int n, int64_t r
     return lo;
 }
 
-// A CTA of the row kernels takes whole rows, about kRowItems pieces of eight elements; 32-bit divisions by a fixed number are a multiplication.
+// A CTA of the row kernels takes whole rows, about kRowItems pieces of eight elements.
 constexpr int kRowItems = 1024, kRowThreads = 256, kMostRows = kRowItems / 4;   // (a row has four pieces at least)
-struct FastDiv {
-    uint32_t by, mul, shift;   // x / by = (x mul) >> (32 + shift), x < 2^24
-    static FastDiv of(uint32_t by)
-    {
-        FastDiv f{by, 0u, 0u};
-        while ((1u << f.shift) < by) ++f.shift;
-        f.mul = (uint32_t)(((uint64_t)1 << 32) * ((1ull << f.shift) - by) / by + 1);   // round-up multiplier less 2^32
-        return f;
-    }
-    __device__ uint32_t div(uint32_t x) const { return (uint32_t)(((uint64_t)__umulhi(x, mul) + x) >> shift); }
-};
 inline int rows_of_cta(int per_row) { return std::max(1, kRowItems / per_row); }
 
 struct AppendParams {

@@ -34,6 +34,19 @@ inline Cache4 cache4_of(const aif_cache4 *c)
     return k;
 }
 
+// 32-bit division by a number that the host knows: a multiplication.
+struct FastDiv {
+    uint32_t by, mul, shift;   // x / by = (x mul) >> (32 + shift)
+    static FastDiv of(uint32_t by)
+    {
+        FastDiv f{by, 0u, 0u};
+        while ((1u << f.shift) < by) ++f.shift;
+        f.mul = (uint32_t)(((uint64_t)1 << 32) * ((1ull << f.shift) - by) / by + 1);   // round-up multiplier less 2^32
+        return f;
+    }
+    __device__ uint32_t div(uint32_t x) const { return (uint32_t)(((uint64_t)__umulhi(x, mul) + x) >> shift); }
+};
+
 int cache4_check(const aif_cache4 *c);   // AIF_OK, AIF_ERR_ARG or AIF_ERR_SHAPE
 int cache4_failed(cudaError_t e, const char *what);
 

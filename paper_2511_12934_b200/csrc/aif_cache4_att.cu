@@ -110,8 +110,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_att4_rows(const AttCall a)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             m[r] = -FLT_MAX, l[r] = 0.f;
-            const int rr = min(r, rows - 1) + r0, query = rr / a.group;
-            const T *src = static_cast<const T *>(a.q) + (e.row0 + query) * a.q_stride + (head * a.group + rr - query * a.group) * d + part * E;
+            const T *src = static_cast<const T *>(a.q) + row_at(a, e.row0, head, min(r, rows - 1) + r0, a.q_stride, d) + part * E;
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 float v[8] = {};
@@ -238,8 +237,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_att4_rows(const AttCall a)
                 sum += from[col] * f, weight += from[d + 1] * f;
             }
             if (begins && ends) {
-                const int rr = r0 + r, query = rr / a.group;
-                T *dst = static_cast<T *>(a.out) + (e.row0 + query) * a.out_stride + (head * a.group + rr - query * a.group) * d + col;
+                T *dst = static_cast<T *>(a.out) + row_at(a, e.row0, head, r0 + r, a.out_stride, d) + col;
                 // (no keys: a zero row; a bad sequence: no number)
                 *dst = (T)(e.length < 0 ? NAN : groups == 0 ? 0.f : sum / weight);
             } else {
@@ -323,8 +321,7 @@ __global__ void __launch_bounds__(256) k_att4_join(const AttCall a, int permuted
             __syncthreads();
         }
         if (work && part == 0 && col < d) {
-            const int rr = h.r0 + r, query = rr / a.group;
-            T *dst = static_cast<T *>(a.out) + (h.row0 + query) * a.out_stride + (h.head * a.group + rr - query * a.group) * d;
+            T *dst = static_cast<T *>(a.out) + row_at(a, h.row0, h.head, h.r0 + r, a.out_stride, d);
             const float v[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -430,7 +427,7 @@ int aif_cache4_attention(const aif_cache4 *c, const aif_cache4_query *q, aif_str
     if (f.cut && (!q->workspace || !at16(q->workspace) || q->workspace_bytes < workspace_of(f, c))) return AIF_ERR_ARG;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     AttCall a{};
-    a.c = cache4_of(c), a.n = q->n, a.n_heads = q->n_heads, a.group = q->n_heads / c->heads, a.seq_ids = q->seq_ids, a.offsets = q->offsets;
+    a.c = cache4_of(c), a.n = q->n, a.n_heads = q->n_heads, a.group = q->n_heads / c->heads, a.by_group = FastDiv::of((uint32_t)a.group), a.seq_ids = q->seq_ids, a.offsets = q->offsets;
     a.rows = q->rows, a.q = q->q, a.out = q->out, a.q_stride = q->q_stride, a.out_stride = q->out_stride;
     a.scale_log2 = 1.4426950408889634f * (q->scale == 0.f ? 1.0f / sqrtf((float)c->d) : q->scale);
     a.window = q->window, a.sinks = q->sinks, a.tile_rows = f.tile_rows, a.block_keys = f.block_keys, a.min_units = f.min_units;

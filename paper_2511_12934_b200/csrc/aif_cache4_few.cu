@@ -160,8 +160,7 @@ __global__ void __launch_bounds__(kFewThreads, (FewCfg<NB, SHARED>::kBlocks)) k_
         float q_scale = 0.f;   // of row g: scale x log2(e) x the power of two that its fp16 values are relative to
         {
             const bool there = g < rows;
-            const int rr = r0 + (there ? g : 0), query = rr / a.group;
-            const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(a.q) + (e.row0 + query) * a.q_stride + (head * a.group + rr - query * a.group) * D + t * (D / 4);
+            const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(a.q) + row_at(a, e.row0, head, r0 + (there ? g : 0), a.q_stride, D) + t * (D / 4);
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 const uint4 x = there ? __ldg(reinterpret_cast<const uint4 *>(src) + i) : make_uint4(0u, 0u, 0u, 0u);
@@ -374,8 +373,7 @@ __global__ void __launch_bounds__(kFewThreads, (FewCfg<NB, SHARED>::kBlocks)) k_
                 }
             }
             if (begins && ends) {
-                const int rr = r0 + r, query = rr / a.group;
-                __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + (e.row0 + query) * a.out_stride + (head * a.group + rr - query * a.group) * D + col;
+                __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + row_at(a, e.row0, head, r0 + r, a.out_stride, D) + col;
                 // (no keys: a zero row; a bad sequence: no number)
                 *dst = (__nv_bfloat16)(e.length < 0 ? NAN : groups == 0 ? 0.f : sum / weight);
             } else {

@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
     uint64_t *s_full = bars + 3 * kS, *p_full = s_full + 4, *pv_done = p_full + 4, *q_full = pv_done + 4;   // [half][buffer]; [half]
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(q_full + 2);
     volatile uint32_t *abort_flag = tmem_slot + 1;
-    float *q_norm = reinterpret_cast<float *>(smOut + C::kOutBytes + 512);   // [256]
+    float *q_norm = reinterpret_cast<float *>(smOut + C::kOutBytes + 512);   // [256], squared
     float2 *k_bound = reinterpret_cast<float2 *>(q_norm + 256);        // [stage][32 rows each]: largest sum of a row's squared scales, largest scale of the values
     __shared__ PlanShared<C::kThreads> plan;
 
@@ -106,36 +106,38 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
             constexpr int kPer = D / 8;   // pieces of 16 bytes of a row
             const int piece = lane % kPer, first = wq * 32 + lane / kPer;   // a warp brings the rows it owns
             unsigned char *q = smQ + x * C::kHalfBytes;
+            uint4 w[kPer];
 #pragma unroll
-            for (int i0 = 0; i0 < kPer; i0 += 8) {
-                uint4 w[8];
+            for (int i = 0; i < kPer; ++i) {
+                const int r = x * 128 + first + i * (32 / kPer);
+                w[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (r < rows) w[i] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + row_at(a, cur.e.row0, head, r0 + r, a.q_stride, D) + piece * 8));
+            }
+            float n2[kPer];   // sums of squares of this lane's pieces
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int r = x * 128 + first + (i0 + i) * (32 / kPer);
-                    w[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (r < rows) {
-                        const int rr = r0 + r, query = rr / a.group;
-                        w[i] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + (cur.e.row0 + query) * a.q_stride +
-                                                                     (head * a.group + rr - query * a.group) * D + piece * 8));
-                    }
-                }
+            for (int i = 0; i < kPer; ++i) {
+                const int r = first + i * (32 / kPer);
+                const uint4 o = make_uint4(__byte_perm(w[i].x, w[i].z, 0x5410), __byte_perm(w[i].x, w[i].z, 0x7632), __byte_perm(w[i].y, w[i].w, 0x5410), __byte_perm(w[i].y, w[i].w, 0x7632));
+                *reinterpret_cast<uint4 *>(q + (piece >> 3) * 16384 + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = o;
+                const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                n2[i] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int r = first + (i0 + i) * (32 / kPer);
-                    const uint4 o = make_uint4(__byte_perm(w[i].x, w[i].z, 0x5410), __byte_perm(w[i].x, w[i].z, 0x7632), __byte_perm(w[i].y, w[i].w, 0x5410), __byte_perm(w[i].y, w[i].w, 0x7632));
-                    *reinterpret_cast<uint4 *>(q + (piece >> 3) * 16384 + r * 128 + (((piece & 7) ^ (r & 7)) << 4)) = o;
-                    const uint32_t ww[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-                    float n2 = 0.f;
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const float lo = __uint_as_float(ww[y] << 16), hi = __uint_as_float(ww[y] & 0xffff0000u);
-                        n2 = fmaf(lo, lo, fmaf(hi, hi, n2));
-                    }
-#pragma unroll
-                    for (int y = 1; y < kPer; y <<= 1) n2 += __shfl_xor_sync(0xffffffffu, n2, y);   // (kPer neighbouring lanes have a row)
-                    if (piece == 0) q_norm[x * 128 + r] = sqrtf(n2);
+                for (int y = 0; y < 4; ++y) {
+                    const float lo = __uint_as_float(ww[y] << 16), hi = __uint_as_float(ww[y] & 0xffff0000u);
+                    n2[i] = fmaf(lo, lo, fmaf(hi, hi, n2[i]));
                 }
             }
+            // kPer neighbouring lanes have kPer rows: each step hands half of a lane's sums over, and the lane of piece i ends with row i
+#pragma unroll
+            for (int y = kPer / 2; y > 0; y >>= 1) {
+                const bool upper = (lane & y) != 0;
+#pragma unroll
+                for (int i = 0; i < y; ++i) {
+                    const float give = upper ? n2[i] : n2[i + y], keep = upper ? n2[i + y] : n2[i];
+                    n2[i] = keep + __shfl_xor_sync(0xffffffffu, give, y);
+                }
+            }
+            q_norm[x * 128 + first + piece * (32 / kPer)] = n2[0];
             fence_proxy_async();
             __syncwarp();   // (the norms are read by the lanes that own the rows)
             mbar_arrive(smem_u32(q_full + x));
@@ -151,25 +153,28 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
             tile_of(cur, head, r0, rows);
             if (rows > x * 128) {
                 float m_used = 0.f, l_sum = 0.f;
-                const float reach = q_norm[x * 128 + row] * k2;   // times a bound of |k|: a bound of the row's scores
+                const float reach = sqrtf(q_norm[x * 128 + row]) * k2;   // times a bound of |k|: a bound of the row's scores
+                uint32_t sc[BN];
+                auto bring_scores = [&](uint32_t n) {
+                    if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(s_full + 2 * x + (n & 1u)), (n >> 1) & 1u, abort_flag))) return false;
+                    tc_fence_after();
+                    tmem_ld32(ts0 + (n & 1u) * BN, *reinterpret_cast<uint32_t(*)[32]>(&sc[0]));
+                    return true;
+                };
                 for (int j = 0; j < take; ++j, ++gb) {
                     const int vc = min(BN, keys - (cur.block + j) * BN);   // keys of the block that exist (none: an empty sequence)
                     const uint32_t b = gb & 1u, ts = ts0 + b * BN;
-                    if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(s_full + 2 * x + b), (gb >> 1) & 1u, abort_flag))) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    uint32_t sc[BN];
-                    tmem_ld32(ts, *reinterpret_cast<uint32_t(*)[32]>(&sc[0]));
-                    tmem_ld32(ts + 32, *reinterpret_cast<uint32_t(*)[32]>(&sc[32]));
+                    // the first half of the block's scores was asked for with the block before; the second comes while the first is at work
+                    if (!(ok = bring_scores(gb))) break;
                     const float4 kb = *reinterpret_cast<const float4 *>(k_bound + (cb + (uint32_t)j) % kS * 2);
                     const float vtop = fmaxf(kb.y, kb.w);
                     // a code is at most 6: |k|^2 <= 36 x 32 x the sum of its blocks' squared scales
                     bool free = reach * 33.9411255f * sqrtf(fmaxf(kb.x, kb.z)) <= kFreeScore && fabsf(m_used) <= kFreeOffset && vtop >= 5.9604645e-8f && vtop <= 256.f;
                     free = __all_sync(0xffffffffu, free);   // (NaN: not)
                     tmem_ld_wait();
+                    tmem_ld32(ts + 32, *reinterpret_cast<uint32_t(*)[32]>(&sc[32]));
                     if (!free) {
+                        tmem_ld_wait();
                         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                         if (vc == BN) {
 #pragma unroll
@@ -212,6 +217,7 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
                     auto probabilities = [&](auto masked) {   // over the scores, as bf16 pairs
 #pragma unroll
                         for (int c0 = 0; c0 < BN; c0 += 32) {
+                            if (c0 == 32) tmem_ld_wait();
                             uint32_t packed[16];
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
@@ -232,6 +238,7 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
                     };
                     if (vc == BN) probabilities(std::false_type{});
                     else probabilities(std::true_type{});
+                    // (the scores of the next block wait for nothing that this one's probabilities have yet to do)
                     tmem_st_wait();
                     float x0, x1, y0, y1;
                     unpack_f32x2(ls2[0], x0, x1), unpack_f32x2(ls2[1], y0, y1);
@@ -250,6 +257,9 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
                 const int r = x * 128 + row;
                 float *rec = a.records + (size_t)(2 * cta + (begins ? 1 : 0)) * 256 * (D + 2);
                 unsigned char *slab = smOut + warp * 2048;
+                int64_t dst[4];   // where the rows that this lane stores begin
+#pragma unroll
+                for (int i = 0; i < 4; ++i) dst[i] = row_at(a, done.e.row0, head, r0 + x * 128 + wq * 32 + i * 8 + (lane >> 2), a.out_stride, D) + (lane & 3) * 8;
 #pragma unroll 1
                 for (int c0 = 0; c0 < D; c0 += 32) {
                     uint32_t v[32];
@@ -272,13 +282,9 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
                         __syncwarp();
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const int rl = i * 8 + (lane >> 2), q = lane & 3, rt = x * 128 + wq * 32 + rl, rr = r0 + rt;
+                            const int rl = i * 8 + (lane >> 2), q = lane & 3;
                             const uint4 o = *reinterpret_cast<const uint4 *>(slab + rl * 64 + ((q ^ ((rl >> 1) & 3)) << 4));
-                            if (rt < rows) {
-                                const int query = rr / a.group;
-                                __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + (done.e.row0 + query) * a.out_stride + (head * a.group + rr - query * a.group) * D + c0 + q * 8;
-                                *reinterpret_cast<uint4 *>(dst) = o;
-                            }
+                            if (x * 128 + wq * 32 + rl < rows) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + dst[i] + c0) = o;
                         }
                         __syncwarp();
                     } else if (r < rows) {

@@ -16,6 +16,7 @@ struct PieceHeader;
 struct AttCall {
     Cache4 c;
     int32_t n, n_heads, group;     // group = n_heads / c.heads
+    FastDiv by_group;
     const int32_t *seq_ids;
     const int64_t *offsets;
     int64_t rows;
@@ -93,6 +94,13 @@ template <int THREADS>
 struct PlanShared {
     int64_t sum[THREADS];   // units before the sequences of every thread
 };
+
+// Elements before row rr (query x group) of head `head` of the cache, for a sequence whose first query row is row0, in q or out.
+__device__ __forceinline__ int64_t row_at(const AttCall &a, int64_t row0, int head, int rr, int64_t stride, int d)
+{
+    const int query = (int)a.by_group.div((uint32_t)rr);
+    return (row0 + query) * stride + (head * a.group + rr - query * a.group) * d;
+}
 
 // x / y for y > 0: in 32 bits where that does (a 64-bit division costs some hundred cycles).
 __device__ __forceinline__ int64_t divide(int64_t x, int64_t y)
