@@ -80,7 +80,12 @@ __device__ __forceinline__ int blocks_at(const AttCall &a, const Entry &e)
     return max(1, a.block_keys > 0 ? (int)(((int64_t)e.keys() + a.block_keys - 1) / a.block_keys) : (e.groups() - a.block_keys - 1) / -a.block_keys);
 }
 __device__ __forceinline__ int tiles_at(const AttCall &a, const Entry &e) { return (e.rows + a.tile_rows - 1) / a.tile_rows; }
-__device__ __forceinline__ int64_t units_at(const AttCall &a, const Entry &e) { return (int64_t)tiles_at(a, e) * a.c.heads * blocks_at(a, e); }
+__device__ __forceinline__ int64_t units_at(const AttCall &a, const Entry &e, int &tiles)
+{
+    const int mine = tiles_at(a, e) * a.c.heads;
+    tiles += mine;
+    return (int64_t)mine * blocks_at(a, e);
+}
 
 // Where a CTA's units begin: entry, tile (head x row tile) and block in it.
 struct Cursor {
@@ -139,12 +144,13 @@ __device__ Share plan_share(const AttCall &a, PlanShared<THREADS> &s)
     const int per = few ? (a.n + 31) >> 5 : (a.n + THREADS - 1) / THREADS, first = (few ? lane : tid) * per;
     int64_t mine = 0, unit[4] = {0, 0, 0, 0};
     bool bad = false;
+    int tiles = 0;
     if (few) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int i = first + j;
             if (j < per && i < a.n) {
-                if (offsets_ok(a, i)) unit[j] = units_at(a, entry_at(a, i));
+                if (offsets_ok(a, i)) unit[j] = units_at(a, entry_at(a, i), tiles);
                 else bad = true;
             }
             mine += unit[j];
@@ -152,7 +158,7 @@ __device__ Share plan_share(const AttCall &a, PlanShared<THREADS> &s)
     } else {
 #pragma unroll 4
         for (int i = first; i < min(a.n, first + per); ++i) {
-            if (offsets_ok(a, i)) mine += units_at(a, entry_at(a, i));
+            if (offsets_ok(a, i)) mine += units_at(a, entry_at(a, i), tiles);
             else bad = true;
         }
     }
@@ -167,15 +173,18 @@ __device__ Share plan_share(const AttCall &a, PlanShared<THREADS> &s)
     if (few) {
         h.total = __shfl_sync(0xffffffffu, x, 31);
         bad = __any_sync(0xffffffffu, bad);
+        tiles = __reduce_add_sync(0xffffffffu, tiles);
     } else {
         __shared__ int64_t warp_sum[THREADS / 32];
-        if (lane == 31) warp_sum[tid >> 5] = x;
+        __shared__ int warp_tiles[THREADS / 32];
+        tiles = __reduce_add_sync(0xffffffffu, tiles);
+        if (lane == 31) warp_sum[tid >> 5] = x, warp_tiles[tid >> 5] = tiles;
         bad = __syncthreads_or(bad) != 0;
         int64_t before = 0;
-        h.total = 0;
+        h.total = 0, tiles = 0;
         for (int w = 0; w < THREADS / 32; ++w) {
             if (w < (tid >> 5)) before += warp_sum[w];
-            h.total += warp_sum[w];
+            h.total += warp_sum[w], tiles += warp_tiles[w];
         }
         base += before;
         s.sum[tid] = base;
@@ -187,7 +196,8 @@ __device__ Share plan_share(const AttCall &a, PlanShared<THREADS> &s)
         if (tid == 0 && cta == 0) atomicOr(a.c.status, AIF_STATUS_BAD_ID);
     }
     if (h.total == 0) return h;
-    h.ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, a.min_units == 1 ? h.total : divide(h.total, a.min_units)));
+    // a CTA has min_units on average at least, or as many as a tile has: tiles beside each other cost nothing to part (148 tiles of one block: 13 us against 35)
+    h.ctas = (int)min((int64_t)gridDim.x, max((int64_t)tiles, a.min_units == 1 ? h.total : divide(h.total, a.min_units)));
     if (cta >= h.ctas) return h;
     h.u0 = cut(h.total, h.ctas, cta), h.u1 = cut(h.total, h.ctas, cta + 1);
     // the sequence of unit u0
@@ -209,7 +219,7 @@ __device__ Share plan_share(const AttCall &a, PlanShared<THREADS> &s)
         }
         i = lo * per, left = h.u0 - s.sum[lo];
         for (; i < a.n - 1; ++i) {
-            const int64_t has = units_at(a, entry_at(a, i));
+            const int64_t has = units_at(a, entry_at(a, i), tiles);
             if (left < has) break;
             left -= has;
         }
