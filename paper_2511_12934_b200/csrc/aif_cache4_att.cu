@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_att4_rows(const AttCall a)
     bool bad_page = false;
     while (u < u1) {
         const Entry &e = cur.e;
-        const int row_tiles = cur.tiles / c.heads, head = cur.tile / row_tiles, r0 = (cur.tile - head * row_tiles) * R, rows = min(R, e.rows - r0);
+        const int head = cur.head, r0 = cur.row_tile * R, rows = min(R, e.rows - r0);
         const int64_t tile_u0 = u - cur.block;
         const int take = (int)min(u1 - u, (int64_t)(cur.blocks - cur.block));
         const int groups = e.groups(), g0 = cur.block * kRowGroups, g1 = min(groups, (cur.block + take) * kRowGroups);
@@ -359,7 +359,8 @@ cudaError_t run_rows(const AttCall &a, int grid, cudaStream_t st)
 // How a call is run: which kernel, and how far it may be cut.
 struct AttForm {
     enum { kRows, kFew, kPair, kTensor } kernel;
-    int tile_rows, block_keys, grid, min_units;
+    int tile_rows, block_keys;   // powers of two; block_keys < 0: that many groups of 16 rows
+    int grid, min_units;
     bool cut;   // a tile may have several units, and so be cut between CTAs
 };
 // The tensor-core kernels: pieces of a cut tile have eight blocks (of some 1.2 us) on average at least, since a piece costs its queries, its record and its part of the join: 16
@@ -433,7 +434,8 @@ int aif_cache4_attention(const aif_cache4 *c, const aif_cache4_query *q, aif_str
     a.c = cache4_of(c), a.n = q->n, a.n_heads = q->n_heads, a.group = q->n_heads / c->heads, a.by_group = FastDiv::of((uint32_t)a.group), a.seq_ids = q->seq_ids, a.offsets = q->offsets;
     a.rows = q->rows, a.q = q->q, a.out = q->out, a.q_stride = q->q_stride, a.out_stride = q->out_stride;
     a.scale_log2 = 1.4426950408889634f * (q->scale == 0.f ? 1.0f / sqrtf((float)c->d) : q->scale);
-    a.window = q->window, a.sinks = q->sinks, a.tile_rows = f.tile_rows, a.block_keys = f.block_keys, a.min_units = f.min_units;
+    a.window = q->window, a.sinks = q->sinks, a.tile_rows = f.tile_rows, a.min_units = f.min_units;
+    a.in_groups = f.block_keys < 0, a.tile_shift = __builtin_ctz((unsigned)f.tile_rows), a.block_shift = __builtin_ctz((unsigned)std::abs(f.block_keys));
     if (f.cut) a.headers = static_cast<PieceHeader *>(q->workspace), a.records = reinterpret_cast<float *>(a.headers + f.grid);
     const bool bf = q->dtype == AIF_BF16, shared = c->shared != 0;
     cudaError_t e;

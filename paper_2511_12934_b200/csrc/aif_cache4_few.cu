@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kFewThreads, (FewCfg<NB, SHARED>::kBlocks)) k_
     bool bad_page = false;
     while (u < u1) {
         const Entry &e = cur.e;
-        const int row_tiles = cur.tiles / c.heads, head = cur.tile / row_tiles, r0 = (cur.tile - head * row_tiles) * kFewRows, rows = min(kFewRows, e.rows - r0);
+        const int head = cur.head, r0 = cur.row_tile * kFewRows, rows = min(kFewRows, e.rows - r0);
         const int64_t tile_u0 = u - cur.block;
         const int take = (int)min(u1 - u, (int64_t)(cur.blocks - cur.block));
         const int groups = e.groups(), g0 = cur.block * kFewGroups, g1 = min(groups, (cur.block + take) * kFewGroups);

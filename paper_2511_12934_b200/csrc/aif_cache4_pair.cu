@@ -16,6 +16,10 @@
 // probabilities lose precision with magnitude.
 // Eight codes of a word come apart as the pairs (0,4) (1,5) (2,6) (3,7) with two shifts, two masks and a multiplication each; queries are put
 // into the same order as they are brought, and sums are taken out of it as they are stored.
+// Bound: what the softmax warps issue and wait for (per 64 keys and half a tile 512 cycles of exponentials in a scheduler, some 1100 in all; a polynomial on other units in
+// place of a quarter or half of the exponentials gained nothing, half of the products left out 1 %), and instruction fetch: five kinds of code share a multiprocessor, so parts
+// stand once and cold ones aside.  16 x 10^4 rows x 10^4 keys, d = 128: 766 us, 1070 TFLOP/s; 148 x 256 x 8192: 151 us, d = 64 134 us, values of their own 181 us; one tile of two
+// blocks 17 us, of which 3 plan, 2.5 queries, 2.3 the output.
 // Rounding: probabilities are rounded to bf16 for the product (relative 2^-9 each), and their sum is of the rounded ones, everything else is fp32.
 #include <cfloat>
 #include <type_traits>
@@ -86,12 +90,10 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
     const Share share = plan_share(a, plan);
     const int64_t total = share.total, u0 = share.u0, u1 = share.u1;
     const int ctas = share.ctas;
-    const bool work = u0 < u1;
     Cursor cur = share.cur;
     int64_t u = u0;
     auto tile_of = [&](const Cursor &at, int &head, int &r0, int &rows) {
-        const int row_tiles = at.tiles / c.heads;
-        head = at.tile / row_tiles, r0 = (at.tile - head * row_tiles) * 256, rows = min(256, at.e.rows - r0);
+        head = at.head, r0 = at.row_tile * 256, rows = min(256, at.e.rows - r0);
     };
 
     if (warp < 8) {
@@ -142,114 +144,20 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
             __syncwarp();   // (the norms are read by the lanes that own the rows)
             mbar_arrive(smem_u32(q_full + x));
         };
-        if (work) bring_queries();
         const uint32_t ts0 = tmem + ((uint32_t)(wq * 32) << 16) + (uint32_t)(C::kTmemS + x * 128), to = tmem + ((uint32_t)(wq * 32) << 16) + (uint32_t)(C::kTmemO + x * D);
         const float k2 = a.scale_log2;
         uint32_t gb = 0, cb = 0;   // blocks of this half; of the CTA, up to the tile's first
-        bool ok = true;
-        while (ok && u < u1) {
-            const int take = (int)min(u1 - u, (int64_t)(cur.blocks - cur.block)), keys = cur.e.keys();
-            int head, r0, rows;
-            tile_of(cur, head, r0, rows);
-            if (rows > x * 128) {
-                float m_used = 0.f, l_sum = 0.f;
-                const float reach = sqrtf(q_norm[x * 128 + row]) * k2;   // times a bound of |k|: a bound of the row's scores
-                uint32_t sc[BN];
-                auto bring_scores = [&](uint32_t n) {
-                    if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(s_full + 2 * x + (n & 1u)), (n >> 1) & 1u, abort_flag))) return false;
-                    tc_fence_after();
-                    tmem_ld32(ts0 + (n & 1u) * BN, *reinterpret_cast<uint32_t(*)[32]>(&sc[0]));
-                    return true;
-                };
-                for (int j = 0; j < take; ++j, ++gb) {
-                    const int vc = min(BN, keys - (cur.block + j) * BN);   // keys of the block that exist (none: an empty sequence)
-                    const uint32_t b = gb & 1u, ts = ts0 + b * BN;
-                    // the first half of the block's scores was asked for with the block before; the second comes while the first is at work
-                    if (!(ok = bring_scores(gb))) break;
-                    const float4 kb = *reinterpret_cast<const float4 *>(k_bound + (cb + (uint32_t)j) % kS * 2);
-                    const float vtop = fmaxf(kb.y, kb.w);
-                    // a code is at most 6: |k|^2 <= 36 x 32 x the sum of its blocks' squared scales
-                    bool free = reach * 33.9411255f * sqrtf(fmaxf(kb.x, kb.z)) <= kFreeScore && fabsf(m_used) <= kFreeOffset && vtop >= 5.9604645e-8f && vtop <= 256.f;
-                    free = __all_sync(0xffffffffu, free);   // (NaN: not)
-                    tmem_ld_wait();
-                    tmem_ld32(ts + 32, *reinterpret_cast<uint32_t(*)[32]>(&sc[32]));
-                    if (!free) {
-                        tmem_ld_wait();
-                        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                        if (vc == BN) {
-#pragma unroll
-                            for (int i = 0; i < BN; i += 8)
-#pragma unroll
-                                for (int q = 0; q < 4; ++q) mx[q] = fmax3(mx[q], __uint_as_float(sc[i + 2 * q]), __uint_as_float(sc[i + 2 * q + 1]));
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < BN; ++i)
-                                if (i < vc) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(sc[i]));
-                        }
-                        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * k2;
-                        if (j == 0) {
-                            m_used = fmaxf(mt, -FLT_MAX);   // finite even where no score is
-                        } else {
-                            const bool need = mt > m_used + 8.0f;
-                            if (__any_sync(0xffffffffu, need)) {
-                                // the exponent's offset follows the maximum only when that has grown by 2^8; this warp's rows of O then
-                                const float m_new = need ? mt : m_used, f = fast_exp2(m_used - m_new);
-                                l_sum *= f, m_used = m_new;
-                                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(pv_done + 2 * x + (b ^ 1u)), ((gb - 1) >> 1) & 1u, abort_flag))) {
-                                    ok = false;
-                                    break;
-                                }
-                                tc_fence_after();
-#pragma unroll 1
-                                for (int c0 = 0; c0 < D; c0 += 16) {
-                                    uint32_t r[16];
-                                    tmem_ld16(to + (uint32_t)c0, r);
-                                    tmem_ld_wait();
-#pragma unroll
-                                    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
-                                    tmem_st16(to + (uint32_t)c0, r);
-                                }
-                            }
-                        }
-                    }
-                    const uint64_t k2p = pack_f32x2(k2, k2), mneg = pack_f32x2(-m_used, -m_used);
-                    uint64_t ls2[2] = {0ull, 0ull};
-                    auto probabilities = [&](auto masked) {   // over the scores, as bf16 pairs
-#pragma unroll
-                        for (int c0 = 0; c0 < BN; c0 += 32) {
-                            if (c0 == 32) tmem_ld_wait();
-                            uint32_t packed[16];
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                float p0, p1;
-                                unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sc[c0 + 2 * i]), __uint_as_float(sc[c0 + 2 * i + 1])), k2p, mneg), p0, p1);
-                                p0 = fast_exp2(p0), p1 = fast_exp2(p1);
-                                if (decltype(masked)::value) {
-                                    if (c0 + 2 * i >= vc) p0 = 0.f;
-                                    if (c0 + 2 * i + 1 >= vc) p1 = 0.f;
-                                }
-                                const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
-                                packed[i] = *reinterpret_cast<const uint32_t *>(&h);
-                                // the sum is of the rounded weights, those that the values get: a row with one heavy key is then as exact as its value
-                                ls2[i & 1] = add_f32x2(ls2[i & 1], pack_f32x2(__uint_as_float(packed[i] << 16), __uint_as_float(packed[i] & 0xffff0000u)));
-                            }
-                            tmem_st16(ts + (uint32_t)(c0 / 2), packed);
-                        }
-                    };
-                    if (vc == BN) probabilities(std::false_type{});
-                    else probabilities(std::true_type{});
-                    // (the scores of the next block wait for nothing that this one's probabilities have yet to do)
-                    tmem_st_wait();
-                    float x0, x1, y0, y1;
-                    unpack_f32x2(ls2[0], x0, x1), unpack_f32x2(ls2[1], y0, y1);
-                    l_sum += (x0 + x1) + (y0 + y1);
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(p_full + 2 * x + b));
-                }
-                if (!ok) break;
-                const Cursor done = cur;
-                u += take, cb += (uint32_t)take;
-                if (u < u1) plan_next(a, cur), bring_queries();   // while the last products run
+        bool ok = true, pending = false;   // pending: the tile `done` has its weights and waits for its last products
+        Cursor done = cur;
+        int done_take = 0;
+        float m_used = 0.f, l_sum = 0.f;
+        // (one round more than there are tiles: the code of every part stands once, instructions are what these warps wait for most)
+        while (ok) {
+            if (u < u1) bring_queries();   // while the last products of the tile before run
+            if (pending) {
+                const int take = done_take, keys = done.e.keys();
+                int head, r0, rows;
+                tile_of(done, head, r0, rows);
                 if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(pv_done + 2 * x + ((gb - 1) & 1u)), ((gb - 1) >> 1) & 1u, abort_flag))) break;
                 tc_fence_after();
                 const bool begins = done.block == 0, ends = done.block + take == done.blocks;
@@ -303,10 +211,104 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
                     a.headers[cta] = h;
                 }
                 if (done.e.length < 0 && tid == 0) atomicOr(c.status, AIF_STATUS_BAD_ID);
-            } else {
-                u += take, cb += (uint32_t)take;
-                if (u < u1) plan_next(a, cur), bring_queries();
             }
+            if (u >= u1) break;
+            const int take = (int)min(u1 - u, (int64_t)(cur.blocks - cur.block)), keys = cur.e.keys();
+            int head, r0, rows;
+            tile_of(cur, head, r0, rows);
+            pending = rows > x * 128;
+            if (pending) {
+                m_used = 0.f, l_sum = 0.f;
+                const float reach = sqrtf(q_norm[x * 128 + row]) * k2;   // times a bound of |k|: a bound of the row's scores
+                uint32_t sc[BN];
+                auto bring_scores = [&](uint32_t n) {
+                    if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(s_full + 2 * x + (n & 1u)), (n >> 1) & 1u, abort_flag))) return false;
+                    tc_fence_after();
+                    tmem_ld32(ts0 + (n & 1u) * BN, *reinterpret_cast<uint32_t(*)[32]>(&sc[0]));
+                    return true;
+                };
+                for (int j = 0; j < take; ++j, ++gb) {
+                    const int vc = min(BN, keys - (cur.block + j) * BN);   // keys of the block that exist (none: an empty sequence)
+                    const uint32_t b = gb & 1u, ts = ts0 + b * BN;
+                    // the first half of the block's scores was asked for with the block before; the second comes while the first is at work
+                    if (!(ok = bring_scores(gb))) break;
+                    const float4 kb = *reinterpret_cast<const float4 *>(k_bound + (cb + (uint32_t)j) % kS * 2);
+                    const float vtop = fmaxf(kb.y, kb.w);
+                    // a code is at most 6: |k|^2 <= 36 x 32 x the sum of its blocks' squared scales
+                    bool free = reach * 33.9411255f * sqrtf(fmaxf(kb.x, kb.z)) <= kFreeScore && fabsf(m_used) <= kFreeOffset && vtop >= 5.9604645e-8f && vtop <= 256.f;
+                    free = __all_sync(0xffffffffu, free);   // (NaN: not)
+                    tmem_ld_wait();
+                    tmem_ld32(ts + 32, *reinterpret_cast<uint32_t(*)[32]>(&sc[32]));
+                    if (__builtin_expect(!free || vc < BN, 0)) {
+                        tmem_ld_wait();
+                        if (vc < BN) {
+#pragma unroll
+                            for (int i = 0; i < BN; ++i)
+                                if (i >= vc) sc[i] = 0xff800000u;   // no key, no weight
+                        }
+                        if (!free) {
+                            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                            for (int i = 0; i < BN; i += 8)
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) mx[q] = fmax3(mx[q], __uint_as_float(sc[i + 2 * q]), __uint_as_float(sc[i + 2 * q + 1]));
+                            const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * k2;
+                            if (j == 0) {
+                                m_used = fmaxf(mt, -FLT_MAX);   // finite even where no score is
+                            } else {
+                                const bool need = mt > m_used + 8.0f;
+                                if (__any_sync(0xffffffffu, need)) {
+                                    // the exponent's offset follows the maximum only when that has grown by 2^8; this warp's rows of O then
+                                    const float m_new = need ? mt : m_used, f = fast_exp2(m_used - m_new);
+                                    l_sum *= f, m_used = m_new;
+                                    if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(pv_done + 2 * x + (b ^ 1u)), ((gb - 1) >> 1) & 1u, abort_flag))) {
+                                        ok = false;
+                                        break;
+                                    }
+                                    tc_fence_after();
+#pragma unroll 1
+                                    for (int c0 = 0; c0 < D; c0 += 16) {
+                                        uint32_t r[16];
+                                        tmem_ld16(to + (uint32_t)c0, r);
+                                        tmem_ld_wait();
+#pragma unroll
+                                        for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+                                        tmem_st16(to + (uint32_t)c0, r);
+                                    }
+                                }
+                            }
+                        }
+                    }
+                    const uint64_t k2p = pack_f32x2(k2, k2), mneg = pack_f32x2(-m_used, -m_used);
+                    uint64_t ls2[2] = {0ull, 0ull};
+                    // probabilities over the scores, as bf16 pairs
+#pragma unroll
+                    for (int c0 = 0; c0 < BN; c0 += 32) {
+                        if (c0 == 32) tmem_ld_wait();
+                        uint32_t packed[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float p0, p1;
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sc[c0 + 2 * i]), __uint_as_float(sc[c0 + 2 * i + 1])), k2p, mneg), p0, p1);
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(fast_exp2(p0), fast_exp2(p1));
+                            packed[i] = *reinterpret_cast<const uint32_t *>(&h);
+                            // the sum is of the rounded weights, those that the values get: a row with one heavy key is then as exact as its value
+                            ls2[i & 1] = add_f32x2(ls2[i & 1], pack_f32x2(__uint_as_float(packed[i] << 16), __uint_as_float(packed[i] & 0xffff0000u)));
+                        }
+                        tmem_st16(ts + (uint32_t)(c0 / 2), packed);
+                    }
+                    tmem_st_wait();
+                    float x0, x1, y0, y1;
+                    unpack_f32x2(ls2[0], x0, x1), unpack_f32x2(ls2[1], y0, y1);
+                    l_sum += (x0 + x1) + (y0 + y1);
+                    tc_fence_before();
+                    mbar_arrive(smem_u32(p_full + 2 * x + b));
+                }
+                if (!ok) break;
+            }
+            done = cur, done_take = take;
+            u += take, cb += (uint32_t)take;
+            if (u < u1) plan_next(a, cur);
         }
     } else if (warp < 10) {
         // ===================== products =====================
@@ -388,7 +390,7 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
             uint4 w[kBlk];
             uint32_t sc;
         };
-        Codes next[C::kKinds];
+        Codes next[C::kKinds] = {};
         bool bad_page = false;
         // The walk runs two of this warp's items ahead for page numbers, one ahead for codes.
         int64_t ahead = u0;
@@ -405,7 +407,7 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
             const int v = cur.block * BN + (int)(item & 1) * 32 + lane;
             if (v >= cur.e.keys()) return;
             const int key = cur.e.key(v);
-            head = c.heads == 1 ? 0 : cur.tile / (cur.tiles / c.heads), in_page = key & (c.page_rows() - 1);
+            head = cur.head, in_page = key & (c.page_rows() - 1);
             page = __ldg(c.table + (size_t)cur.e.seq * c.max_pages + (key >> c.page_shift));
         };
         auto fetch = [&]() {
@@ -425,41 +427,47 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
                 next[k].sc = kBlk == 2 ? (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(ps)) : __ldg(reinterpret_cast<const uint32_t *>(ps));
             }
         };
-        int64_t item = warp - 10;
-        place(item), fetch(), place(item + kUnpackers);
-        for (; item < items; item += kUnpackers) {
+        // (two rounds before the first item: the code of every part stands once)
+        for (int64_t item = warp - 10 - 2 * kUnpackers; item < items; item += kUnpackers) {
+            const bool begun = item >= 0;
             const uint32_t gb = (uint32_t)(item >> 1);
             const int s = (int)(gb % kS), r = (int)(item & 1) * 32 + lane;
-            if (!mbar_wait(smem_u32(kv_empty + s), ((gb / kS) & 1u) ^ 1u, abort_flag)) break;
+            if (begun && !__all_sync(0xffffffffu, mbar_wait(smem_u32(kv_empty + s), ((gb / kS) & 1u) ^ 1u, abort_flag))) break;
 #pragma unroll
             for (int k = 0; k < C::kKinds; ++k) {
-                unsigned char *tile = smKV + s * C::kStageBytes + k * C::kTileBytes + r * 128;
+                if (begun) {
+                    if (k == 0) {
+                        // bounds of the rows
+                        float sum = 0.f, vtop = 0.f;
 #pragma unroll
-                for (int b = 0; b < kBlk; ++b) {
-                    const UnpackScale us((next[k].sc >> (8 * b)) & 255u);
-                    unsigned char *chunk = tile + (b >> 1) * C::kChunkBytes;
-                    const uint32_t w[4] = {next[k].w[b].x, next[k].w[b].y, next[k].w[b].z, next[k].w[b].w};
-#pragma unroll
-                    for (int i4 = 0; i4 < 4; ++i4) *reinterpret_cast<uint4 *>(chunk + ((((b & 1) * 4 + i4) ^ (r & 7)) << 4)) = unpack8(w[i4], us);
-                }
-                // bounds of the rows, before the codes' registers are given away
-                if (k == 0) {
-                    float sum = 0.f;
-#pragma unroll
-                    for (int b = 0; b < kBlk; ++b) {
-                        const float f = mx_scale((next[0].sc >> (8 * b)) & 255u);
-                        sum = fmaf(f, f, sum);
+                        for (int b = 0; b < kBlk; ++b) {
+                            const float f = mx_scale((next[0].sc >> (8 * b)) & 255u);
+                            sum = fmaf(f, f, sum), vtop = fmaxf(vtop, mx_scale((next[C::kKinds - 1].sc >> (8 * b)) & 255u));
+                        }
+                        // (as integers: NaN stays the largest)
+                        const uint32_t st = __reduce_max_sync(0xffffffffu, __float_as_uint(sum)), vt = __reduce_max_sync(0xffffffffu, __float_as_uint(vtop));
+                        if (lane == 0) k_bound[s * 2 + (item & 1)] = make_float2(__uint_as_float(st), __uint_as_float(vt));
                     }
-                    float vtop = 0.f;
+                    // A block of 32 at a time, its codes moved to the front: a loop of a quarter of the instructions, since the warps of a multiprocessor's quarter run different
+                    // code and wait for it (16 x 10^4 x 10^4, d = 128: 784 us against 916; with values of their own, 148 x 256 x 8192: 181 us against 213)
+                    unsigned char *tile = smKV + s * C::kStageBytes + k * C::kTileBytes + r * 128;
+#pragma unroll 1
+                    for (int b = 0; b < kBlk; ++b) {
+                        const UnpackScale us(next[k].sc & 255u);
+                        unsigned char *chunk = tile + (b >> 1) * C::kChunkBytes;
+                        const uint32_t w[4] = {next[k].w[0].x, next[k].w[0].y, next[k].w[0].z, next[k].w[0].w};
 #pragma unroll
-                    for (int b = 0; b < kBlk; ++b) vtop = fmaxf(vtop, mx_scale((next[C::kKinds - 1].sc >> (8 * b)) & 255u));
-                    // (as integers: NaN stays the largest)
-                    const uint32_t st = __reduce_max_sync(0xffffffffu, __float_as_uint(sum)), vt = __reduce_max_sync(0xffffffffu, __float_as_uint(vtop));
-                    if (lane == 0) k_bound[s * 2 + (item & 1)] = make_float2(__uint_as_float(st), __uint_as_float(vt));
+                        for (int i4 = 0; i4 < 4; ++i4) *reinterpret_cast<uint4 *>(chunk + ((((b & 1) * 4 + i4) ^ (r & 7)) << 4)) = unpack8(w[i4], us);
+#pragma unroll
+                        for (int i = 1; i < kBlk; ++i) next[k].w[i - 1] = next[k].w[i];
+                        next[k].sc >>= 8;
+                    }
                 }
                 if (k == C::kKinds - 1) fetch();   // the codes have been used: the next item's may come
-                fence_proxy_async();
-                mbar_arrive(smem_u32((k == 0 ? k_full : v_full) + s));
+                if (begun) {
+                    fence_proxy_async();
+                    mbar_arrive(smem_u32((k == 0 ? k_full : v_full) + s));
+                }
             }
             place(item + 2 * kUnpackers);
         }

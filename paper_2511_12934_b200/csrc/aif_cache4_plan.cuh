@@ -1,7 +1,7 @@
 // Division of an attention call over the 4-bit cache among the CTAs of a launch, worked out on the device: lengths, offsets and page
 // tables are device memory, so a captured call follows them.
 //
-// A tile is up to `tile_rows` query rows (row = query x heads of a group) of one sequence and one head of the cache; a unit is one block of `block_keys`
+// A tile is up to `tile_rows` query rows (row = query x heads of a group) of one sequence and one head of the cache; a unit is one block of a fixed number of
 // visible keys of a tile (an empty sequence has one).  The units of all tiles, one after the other, are cut into equal ranges, one per CTA, so a launch
 // is even whatever the lengths.  A tile that is cut leaves its pieces in the workspace: every CTA has two records, [2 c] for a piece of
 // a tile that began in an earlier CTA and [2 c + 1] for the beginning of one that goes on in the next, and a header that says which tile ends in it.
@@ -25,7 +25,7 @@ struct AttCall {
     int64_t q_stride, out_stride;
     float scale_log2;              // scale x log2(e)
     int32_t window, sinks;
-    int32_t tile_rows, block_keys, min_units;
+    int32_t tile_rows, min_units, tile_shift, block_shift, in_groups;   // tiles and blocks by shifts; in_groups: blocks are of groups of 16 rows
     float *records;                // [2 x grid][tile_rows][d] sums, then [tile_rows][2]: exponent offset and weight
     PieceHeader *headers;          // [grid]; nullptr where no tile can have more than one unit
 };
@@ -74,12 +74,11 @@ __device__ __forceinline__ Entry entry_at(const AttCall &a, int i)
     if (a.window > 0 && e.length > a.window) e.rest = e.length - a.window, e.first = min(a.sinks, e.rest);
     return e;
 }
-// (block_keys < 0: blocks of that many groups of 16 rows)
 __device__ __forceinline__ int blocks_at(const AttCall &a, const Entry &e)
 {
-    return max(1, a.block_keys > 0 ? (int)(((int64_t)e.keys() + a.block_keys - 1) / a.block_keys) : (e.groups() - a.block_keys - 1) / -a.block_keys);
+    return max(1, (int)(((uint32_t)(a.in_groups ? e.groups() : e.keys()) + (1u << a.block_shift) - 1) >> a.block_shift));
 }
-__device__ __forceinline__ int tiles_at(const AttCall &a, const Entry &e) { return (e.rows + a.tile_rows - 1) / a.tile_rows; }
+__device__ __forceinline__ int tiles_at(const AttCall &a, const Entry &e) { return (int)(((uint32_t)e.rows + (1u << a.tile_shift) - 1) >> a.tile_shift); }
 __device__ __forceinline__ int64_t units_at(const AttCall &a, const Entry &e, int &tiles)
 {
     const int mine = tiles_at(a, e) * a.c.heads;
@@ -87,11 +86,11 @@ __device__ __forceinline__ int64_t units_at(const AttCall &a, const Entry &e, in
     return (int64_t)mine * blocks_at(a, e);
 }
 
-// Where a CTA's units begin: entry, tile (head x row tile) and block in it.
+// Where a CTA's units begin: entry, tile (head, then tile of query rows) and block in it.
 struct Cursor {
-    int32_t i, tile, block;
+    int32_t i, head, row_tile, block;
     Entry e;
-    int32_t tiles, blocks;   // of the entry (tiles of all heads)
+    int32_t row_tiles, blocks;   // of the entry (tiles of one head)
 };
 
 // Shared memory of the division.
@@ -226,21 +225,25 @@ __device__ Share plan_share(const AttCall &a, PlanShared<THREADS> &s)
     }
     Cursor &c = h.cur;
     c.i = i, c.e = entry_at(a, i);
-    c.tiles = tiles_at(a, c.e) * a.c.heads, c.blocks = blocks_at(a, c.e);
-    c.tile = (int)divide(left, c.blocks), c.block = (int)(left - (int64_t)c.tile * c.blocks);
+    c.row_tiles = tiles_at(a, c.e), c.blocks = blocks_at(a, c.e);
+    const int tile = (int)divide(left, c.blocks);
+    c.block = (int)(left - (int64_t)tile * c.blocks);
+    c.head = a.c.heads == 1 ? 0 : tile / c.row_tiles, c.row_tile = tile - c.head * c.row_tiles;
     return h;
 }
 // To the next tile (block 0 of it).
 __device__ __forceinline__ void plan_next(const AttCall &a, Cursor &c)
 {
     c.block = 0;
-    if (++c.tile < c.tiles) return;
-    c.tile = 0;
+    if (++c.row_tile < c.row_tiles) return;
+    c.row_tile = 0;
+    if (++c.head < a.c.heads) return;
+    c.head = 0;
     do {
         if (++c.i >= a.n) return;
         c.e = entry_at(a, c.i);
-        c.tiles = tiles_at(a, c.e) * a.c.heads;
-    } while (c.tiles == 0);
+        c.row_tiles = tiles_at(a, c.e);
+    } while (c.row_tiles == 0);
     c.blocks = blocks_at(a, c.e);
 }
 

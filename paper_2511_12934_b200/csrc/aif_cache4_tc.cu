@@ -90,11 +90,9 @@ __global__ void __launch_bounds__(512, 1) k_att4_tc(const AttCall a)
 
     // One query row of the tile that `at` stands on, 16 bytes (piece p of D / 8) into a query buffer, in the order of the unpacked codes.
     auto query_piece = [&](const Cursor &at, int r, int p) -> uint4 {
-        const int row_tiles = at.tiles / c.heads, head = at.tile / row_tiles, r0 = (at.tile - head * row_tiles) * 128;
-        if (r0 + r >= at.e.rows) return make_uint4(0u, 0u, 0u, 0u);
-        const int rr = r0 + r, query = rr / a.group;
-        const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(a.q) + (at.e.row0 + query) * a.q_stride + (head * a.group + rr - query * a.group) * D + p * 8;
-        return __ldg(reinterpret_cast<const uint4 *>(src));
+        const int rr = at.row_tile * 128 + r;
+        if (rr >= at.e.rows) return make_uint4(0u, 0u, 0u, 0u);
+        return __ldg(reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(a.q) + row_at(a, at.e.row0, at.head, rr, a.q_stride, D) + p * 8));
     };
     auto put_query = [&](unsigned char *q, int r, int p, uint4 w) {
         const uint4 o = make_uint4(__byte_perm(w.x, w.z, 0x5410), __byte_perm(w.x, w.z, 0x7632), __byte_perm(w.y, w.w, 0x5410), __byte_perm(w.y, w.w, 0x7632));
@@ -230,11 +228,14 @@ __global__ void __launch_bounds__(512, 1) k_att4_tc(const AttCall a)
             }
             tc_fence_after();
             const float weight = l_sum + l_s[(half ^ 1) * 128 + row];
-            const int row_tiles = cur.tiles / c.heads, head = cur.tile / row_tiles, r0 = (cur.tile - head * row_tiles) * 128, rows = min(128, cur.e.rows - r0);
+            const int head = cur.head, r0 = cur.row_tile * 128, rows = min(128, cur.e.rows - r0);
             const bool begins = cur.block == 0, ends = cur.block + take == cur.blocks;
             const float inv = cur.e.length < 0 ? NAN : keys == 0 ? 0.f : 1.0f / weight;
             float *rec = a.records + (size_t)(2 * cta + (begins ? 1 : 0)) * 128 * (D + 2);
             unsigned char *slab = smOut + warp * 2048;
+            int64_t dst[4];   // where the rows that this lane stores begin
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dst[i] = row_at(a, cur.e.row0, head, r0 + wq * 32 + i * 8 + (lane >> 2), a.out_stride, D) + (lane & 3) * 8;
 #pragma unroll 1
             for (int c0 = half * (D / 2); c0 < (half + 1) * (D / 2); c0 += 32) {
                 uint32_t r[32];
@@ -257,13 +258,9 @@ __global__ void __launch_bounds__(512, 1) k_att4_tc(const AttCall a)
                     __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int rl = i * 8 + (lane >> 2), q = lane & 3, rr = r0 + wq * 32 + rl;
+                        const int rl = i * 8 + (lane >> 2), q = lane & 3;
                         const uint4 o = *reinterpret_cast<const uint4 *>(slab + rl * 64 + ((q ^ ((rl >> 1) & 3)) << 4));
-                        if (wq * 32 + rl < rows) {
-                            const int query = rr / a.group;
-                            __nv_bfloat16 *dst = static_cast<__nv_bfloat16 *>(a.out) + (cur.e.row0 + query) * a.out_stride + (head * a.group + rr - query * a.group) * D + c0 + q * 8;
-                            *reinterpret_cast<uint4 *>(dst) = o;
-                        }
+                        if (wq * 32 + rl < rows) *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.out) + dst[i] + c0) = o;
                     }
                     __syncwarp();
                 } else if (row < rows) {
@@ -396,7 +393,7 @@ __global__ void __launch_bounds__(512, 1) k_att4_tc(const AttCall a)
             const int v = w.at.block * BN + r;
             if (v >= w.at.e.keys()) return;
             const int key = w.at.e.key(v);
-            head = w.at.tile / (w.at.tiles / c.heads), in_page = key & (c.page_rows() - 1);
+            head = w.at.head, in_page = key & (c.page_rows() - 1);
             page = __ldg(c.table + (size_t)w.at.e.seq * c.max_pages + (key >> c.page_shift));
             if (!c.holds(page)) page = -2;
         };
