@@ -4,6 +4,7 @@
 // moves them, bound by HBM.  The books are kept by one CTA, or for many pages one cluster of CTAs: its phases hand over through
 // barriers, a matter of a microsecond, where separate launches would cost two or three each.  Nothing depends on the order of atomics: pages are
 // handed out and taken back by position in the call (prefix sums), so the same calls leave the same books.
+#include <algorithm>
 #include <cstdio>
 
 #include "aif_cache4.cuh"
@@ -520,7 +521,13 @@ __device__ __forceinline__ int entry_of(const int64_t *offsets, int n, int64_t r
 
 // A CTA of the row kernels takes whole rows, about kRowItems pieces of eight elements.
 constexpr int kRowItems = 1024, kRowThreads = 256, kMostRows = kRowItems / 4;   // (a row has four pieces at least)
-inline int rows_of_cta(int per_row) { return std::max(1, kRowItems / per_row); }
+// Of a call with `rows` rows: as many as spread over eight CTAs of every multiprocessor, between that and kMostRows, since a CTA's rows wait for a search and three loads that need
+// one another (read of 944919 rows, d = 128: 77 us with 256 rows to a CTA, 88 with 64).
+inline int rows_of_cta(int per_row, int64_t rows)
+{
+    const int least = std::max(1, kRowItems / per_row), most = std::min(kMostRows, 8 * least);
+    return (int)std::clamp<int64_t>((rows + 148 * 8 - 1) / (148 * 8), least, most);
+}
 
 struct AppendParams {
     Cache4 c;
@@ -832,7 +839,7 @@ int check_rows(const aif_cache4 *c, const void *k, const void *v, int32_t dtype,
 {
     if (dtype != AIF_F32 && dtype != AIF_BF16) return AIF_ERR_ARG;
     if (rows < 0 || rows > (int64_t)1 << 40 || stride < (int64_t)c->heads * c->d || stride > (int64_t)1 << 31) return AIF_ERR_SHAPE;
-    if (rows / rows_of_cta(c->heads * c->d / 8) > INT_MAX - 1024) return AIF_ERR_SHAPE;   // CTAs of a grid
+    if (rows / rows_of_cta(c->heads * c->d / 8, rows) > INT_MAX - 1024) return AIF_ERR_SHAPE;   // CTAs of a grid
     const unsigned el = dtype == AIF_BF16 ? 2 : 4;
     if ((c->shared != 0) != (v == nullptr)) return AIF_ERR_ARG;
     if (rows > 0 && (!k || reinterpret_cast<uintptr_t>(k) % el != 0 || (v && reinterpret_cast<uintptr_t>(v) % el != 0))) return AIF_ERR_ARG;
@@ -925,7 +932,7 @@ int aif_cache4_append(const aif_cache4 *c, int32_t n, const int32_t *seq_ids, co
     if (e == cudaSuccess && rows > 0) {
         AppendParams p{};
         p.c = b.c, p.n = n, p.seq_ids = seq_ids, p.offsets = offsets, p.x[0] = k, p.x[1] = v, p.rows = rows, p.stride = stride;
-        p.per_row = FastDiv::of(c->heads * c->d / 8), p.per_head = FastDiv::of(c->d / 8), p.cta_rows = rows_of_cta(c->heads * c->d / 8);
+        p.per_row = FastDiv::of(c->heads * c->d / 8), p.per_head = FastDiv::of(c->d / 8), p.cta_rows = rows_of_cta(c->heads * c->d / 8, rows);
         p.row_blocks = (int)grid_for(rows, p.cta_rows, INT_MAX);
         const dim3 grid((unsigned)p.row_blocks + grid_for(n, 8, 148), c->shared ? 1 : 2);
         const int el = dtype == AIF_BF16 ? 2 : 4;
@@ -995,7 +1002,7 @@ int aif_cache4_read(const aif_cache4 *c, int32_t n, const int32_t *seq_ids, cons
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     ReadParams p{};
     p.c = cache4_of(c), p.n = n, p.seq_ids = seq_ids, p.offsets = offsets, p.out[0] = k_out, p.out[1] = v_out, p.rows = rows, p.stride = stride;
-    p.per_row = FastDiv::of(c->heads * c->d / 8), p.per_head = FastDiv::of(c->d / 8), p.cta_rows = rows_of_cta(c->heads * c->d / 8);
+    p.per_row = FastDiv::of(c->heads * c->d / 8), p.per_head = FastDiv::of(c->d / 8), p.cta_rows = rows_of_cta(c->heads * c->d / 8, rows);
     const dim3 grid(grid_for(rows, p.cta_rows, INT_MAX), c->shared ? 1 : 2);
     const int el = dtype == AIF_BF16 ? 2 : 4;
     const bool al = at16(k_out) && at16(v_out) && stride * el % 16 == 0;
