@@ -79,11 +79,12 @@ __device__ __forceinline__ int blocks_at(const AttCall &a, const Entry &e)
     return max(1, (int)(((uint32_t)(a.in_groups ? e.groups() : e.keys()) + (1u << a.block_shift) - 1) >> a.block_shift));
 }
 __device__ __forceinline__ int tiles_at(const AttCall &a, const Entry &e) { return (int)(((uint32_t)e.rows + (1u << a.tile_shift) - 1) >> a.tile_shift); }
+// (tiles: their number so far, as far as it matters: up to the CTAs of a launch)
 __device__ __forceinline__ int64_t units_at(const AttCall &a, const Entry &e, int &tiles)
 {
-    const int mine = tiles_at(a, e) * a.c.heads;
-    tiles += mine;
-    return (int64_t)mine * blocks_at(a, e);
+    const int64_t mine = (int64_t)tiles_at(a, e) * a.c.heads;
+    tiles = min(tiles + (int)min(mine, (int64_t)1024), 1024);
+    return mine * blocks_at(a, e);
 }
 
 // Where a CTA's units begin: entry, tile (head, then tile of query rows) and block in it.
