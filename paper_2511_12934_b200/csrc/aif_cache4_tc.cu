@@ -12,6 +12,8 @@
 //          meanwhile, and the page numbers for the one after that
 // Eight codes of a word come apart as the pairs (0,4) (1,5) (2,6) (3,7) with two shifts, two masks and a multiplication each; queries are put
 // into the same order as they are brought, and sums are taken out of it as they are stored.
+// Bound: the unpacking warps and, with shared-memory operands of 64 keys x 256, the products: 148 tiles x 8192 keys 181 us (880 TFLOP/s; values of their own 326 us), 16 x 10^4 rows x
+// 10^4 keys 1.97 ms (832 TFLOP/s), one tile of two blocks 16 us.
 // Rounding: probabilities are rounded to bf16 for the product (relative 2^-9 each), and their sum is of the rounded ones, everything else is fp32.
 #include <cfloat>
 
