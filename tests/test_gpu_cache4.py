@@ -433,6 +433,40 @@ def test_captured_calls_follow_the_cache(dtype, d, rows):
     g.reset()
 
 
+@pytest.mark.parametrize("n", [40, 150])
+def test_captured_books(n):
+    """Fork, append, free and read in one graph, replayed, against the same calls one by one."""
+    rows = torch.randn(5 * n, 64, device="cuda").bfloat16()
+    first, second, off = ids(*range(n)), ids(*range(n, 2 * n)), offsets([5] * n)
+
+    def calls(c, out):
+        c.fork(first, second)
+        c.append(first, off, rows)
+        c.read(second, off, out)
+        c.free(second)
+
+    caches = [B.Cache4(d=64, n_pages=4 * n, page_rows=16, n_seqs=2 * n, max_pages=4) for _ in range(2)]
+    outs = [torch.zeros(5 * n, 64, dtype=torch.bfloat16, device="cuda") for _ in caches]
+    for c in caches:
+        c.append(first, off, rows)
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(g, stream=s):
+            calls(caches[0], outs[0])
+    torch.cuda.synchronize()
+    for _ in range(6):
+        g.replay()
+        torch.cuda.synchronize()
+        calls(caches[1], outs[1])
+        a, b = caches
+        for name in ("table", "lengths", "refs", "n_free"):
+            assert torch.equal(getattr(a, name), getattr(b, name)), name
+        assert torch.equal(a.free_pages[:a.n_free.item()], b.free_pages[:b.n_free.item()]) and torch.equal(outs[0], outs[1])
+    assert a.lengths.tolist() == [35] * n + [0] * n and a.poll_status() == 0 and b.poll_status() == 0
+    g.reset()
+
+
 def test_calls_on_two_streams_side_by_side():
     """Readers of one cache at the same time, each with a workspace of its own."""
     c, k, v = filled([3000, 2500], 128)
