@@ -3,6 +3,7 @@ import glob
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -26,16 +27,17 @@ def _stale() -> bool:
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
-    objs = []
-    for src in sources():
+    def compile_one(src: str) -> str:
         obj = os.path.join(CSRC, os.path.basename(src)[:-3] + ".o")
-        cmd = ["nvcc"] + NVCC_FLAGS + ["-c", src, "-o", obj]
-        r = subprocess.run(cmd, capture_output=True, text=True)
+        r = subprocess.run(["nvcc"] + NVCC_FLAGS + ["-c", src, "-o", obj], capture_output=True, text=True)
         if verbose or r.returncode != 0:
             sys.stderr.write(r.stdout + r.stderr)
         if r.returncode != 0:
             raise RuntimeError(f"nvcc failed on {src}")
-        objs.append(obj)
+        return obj
+
+    with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:   # one nvcc per source, side by side
+        objs = list(pool.map(compile_one, sources()))
     cmd = ["nvcc", "-shared", "-o", LIB] + objs   # static cudart; driver entry points are looked up at run time
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
