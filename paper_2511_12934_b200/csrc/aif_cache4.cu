@@ -10,6 +10,7 @@
 #include <cstdio>
 
 #include "aif_cache4.cuh"
+#include "aif_span.h"
 #include "aif_tc_ptx.cuh"
 
 namespace aif {
@@ -570,8 +571,8 @@ __global__ void __launch_bounds__(kRowThreads) k_append(const AppendParams p)
         }
         return;
     }
-    const int64_t row0 = (int64_t)blockIdx.x * p.cta_rows, all = min(p.offsets[p.n], p.rows);
-    const int rows = (int)min((int64_t)p.cta_rows, all - row0), items = rows * (int)p.per_row.by;
+    const int64_t row0 = (int64_t)blockIdx.x * p.cta_rows;
+    const int rows = rows_before(min(p.offsets[p.n], p.rows), row0, p.cta_rows), items = rows * (int)p.per_row.by;   // (offsets that k_books refused come here too)
     if (rows <= 0) return;
     const T *x = static_cast<const T *>(p.x[which]) + row0 * p.stride;
     for (int i0 = 0; i0 < items; i0 += 4 * kRowThreads) {
@@ -640,7 +641,7 @@ __global__ void __launch_bounds__(kRowThreads) k_read(const ReadParams p)
         return;
     }
     const int64_t row0 = (int64_t)blockIdx.x * p.cta_rows;
-    const int rows = (int)min((int64_t)p.cta_rows, p.offsets[p.n] - row0), items = rows * (int)p.per_row.by;
+    const int rows = rows_before(p.offsets[p.n], row0, p.cta_rows), items = rows * (int)p.per_row.by;
     if (rows <= 0) return;
     if (tid < rows) {
         const int64_t r = row0 + tid;
