@@ -83,9 +83,21 @@ __device__ __forceinline__ uint32_t top_scale(const RowCodes<NB> &r)
     if constexpr (NB == 4) return of_word(r.sc[0]);
     if constexpr (NB == 8) return max(of_word(r.sc[0]), of_word(r.sc[1]));
 }
-// fp16 pair of 2^(byte - top), 0 below 2^-24.  (The byte that stands for NaN makes the row's score NaN by itself: see row_scale.)
+// The same of the blocks that are numbers (separate values: a block of no numbers is one in its own columns only, so the row's weight stays finite).
+template <int NB>
+__device__ __forceinline__ uint32_t top_number(RowCodes<NB> r)
+{
+#pragma unroll
+    for (int i = 0; i < (NB + 3) / 4; ++i)
+#pragma unroll
+        for (int b = 0; b < 32; b += 8)
+            if (((r.sc[i] >> b) & 255u) == kMxNan) r.sc[i] &= ~(255u << b);
+    return top_scale<NB>(r);
+}
+// fp16 pair of 2^(byte - top), 0 below 2^-24; NaN for a block that is none.
 __device__ __forceinline__ uint32_t relative_scale(uint32_t byte, uint32_t top)
 {
+    if (byte == kMxNan) return 0x7fff7fffu;
     const float f = __uint_as_float((uint32_t)max((int)(127u + byte) - (int)top, 0) << 23);
     return pack_f16x2(f, f);
 }
@@ -285,10 +297,10 @@ __global__ void __launch_bounds__(kFewThreads, (FewCfg<NB, SHARED>::kBlocks)) k_
                     const uint32_t top = top_scale<NB>(kr[h]);
                     unpack_row<NB>(kr[h], top, t, kf[x][h]);
                     scale[x][h] = row_scale(top);
-                    // the exponent of the values' scale; a row of no numbers is one in its weights
+                    // the exponent of the values' scale
                     uint32_t vtop = top;
-                    if constexpr (!SHARED) vtop = top_scale<NB>(vc[x][h]);
-                    v_exp[x][h] = !SHARED && vtop == kMxNan ? NAN : (float)(int)vtop;
+                    if constexpr (!SHARED) vtop = top_number<NB>(vc[x][h]);
+                    v_exp[x][h] = (float)(int)vtop;
                 }
             }
             bool raise = false;
@@ -333,7 +345,7 @@ __global__ void __launch_bounds__(kFewThreads, (FewCfg<NB, SHARED>::kBlocks)) k_
                 const uint32_t p0 = transpose8(pack_f16x2(w[x][0], w[x][1])), p1 = transpose8(pack_f16x2(w[x][2], w[x][3]));
                 if constexpr (!SHARED) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) unpack_row<NB>(vc[x][h], top_scale<NB>(vc[x][h]), t, kf[x][h]);
+                    for (int h = 0; h < 2; ++h) unpack_row<NB>(vc[x][h], top_number<NB>(vc[x][h]), t, kf[x][h]);
                 }
 #pragma unroll
                 for (int i = 0; i < KS; ++i)

@@ -1,8 +1,11 @@
 """The 4-bit sequence cache on the GPU at its borders: lists of offsets that are none, numbers of any size."""
+import math
+
 import pytest
 import torch
 
 from paper_2511_12934_b200 import binding as B
+from tests import mx4_reference as R
 from tests.test_gpu_cache4 import filled, ids, offsets
 
 pytestmark = pytest.mark.gpu
@@ -31,3 +34,36 @@ def test_append_with_bad_offsets_leaves_everything(n, dtype, shared):
         assert torch.equal(getattr(c, name), before[name]), name
     c.append(ids(*range(n)), off, *rows)
     assert c.poll_status() == 0 and c.lengths.tolist() == [(11 * i) % 60 + 5 for i in range(n)]
+
+
+# every kernel: fp32 by one and by four rows, bf16 of few rows, of many by d
+KERNELS = [(torch.float32, 128, 1), (torch.float32, 64, 5), (torch.bfloat16, 32, 2), (torch.bfloat16, 64, 3), (torch.bfloat16, 128, 9), (torch.bfloat16, 256, 2), (torch.bfloat16, 96, 2),
+           (torch.bfloat16, 160, 7), (torch.bfloat16, 64, 100), (torch.bfloat16, 128, 300), (torch.bfloat16, 256, 60)]
+
+
+def hold(q, k, v, out, columns=slice(None)):
+    """out [rows, 1, d] of a call with scale 1 / sqrt(d) over all of k, v [keys, d] (float64) against the reference, in these columns."""
+    d = k.shape[1]
+    for r in range(0, q.shape[0], max(1, q.shape[0] // 5)):
+        ref, spread, mass, reach = R.attention(q[r].double(), k, v, 1 / math.sqrt(d))
+        bound = R.attention_bound(q.dtype, ref, spread, mass, reach, d)
+        err = (out[r].double() - ref).abs()
+        assert (err <= bound)[:, columns].all(), (r, (err / bound)[:, columns].max().item())
+
+
+@pytest.mark.parametrize("dtype, d, rows", KERNELS)
+def test_a_block_of_values_that_is_no_number_spoils_its_columns_alone(dtype, d, rows):
+    """Values of their own: an infinity in row 40 makes one block of 32 values NaN, which reaches those 32 columns of every output and no other."""
+    n, block = 90, d // 32 - 1
+    g = torch.Generator(device="cuda").manual_seed(d)
+    k, v = [torch.randn(n, 1, d, generator=g, device="cuda") * 0.3 for _ in range(2)]
+    v[40, 0, 32 * block + 5] = math.inf
+    c = B.Cache4(d=d, n_pages=8, page_rows=16, n_seqs=1, max_pages=8, shared=False)
+    c.append(ids(0), offsets([n]), k, v)
+    q = (torch.randn(rows, 1, d, generator=g, device="cuda") * 4).to(dtype)
+    out = c.attention(q, torch.empty_like(q), offsets=offsets([rows]))
+    spoilt = torch.zeros(d, dtype=torch.bool, device="cuda")
+    spoilt[32 * block:] = True
+    assert torch.equal(torch.isnan(out), spoilt.expand_as(out)) and c.poll_status() == 0
+    kq, vq = R.quantise(k)[0][:, 0], torch.nan_to_num(R.quantise(v)[0][:, 0])
+    hold(q, kq, vq, out, ~spoilt)
