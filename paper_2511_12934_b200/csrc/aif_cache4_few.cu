@@ -1,16 +1,15 @@
 // Attention of up to eight query rows (queries x heads of a group) of a sequence in the 4-bit cache, bf16, d = 32, 64, 128, 256, where the work is to read
-// the cache once: warp-level tensor-core products, fp16 operands, fp32 sums.
+// the cache once: warp-level tensor-core products, bf16 operands, fp32 sums.
 //
 // A warp takes 16 keys at a time, one group of 16 rows of a page.  Lane (g, t) = (lane / 4, lane % 4) reads a quarter of the rows g and g + 8 and unpacks it to
-// fp16 relative to the row's largest scale (exact down to 2^-23 of it).  Those registers are the A operand of scores^T [16 keys x 8 rows] = K Q^T (the
-// order of the columns is the lanes' own, the same for keys and queries) and, transposed 8 x 8 by movmatrix, of O^T [d x 8 rows] += V^T P^T, so a row is
-// read and unpacked once where values are the keys.  The row's scale 2^E_j goes into its weight: weights are exp2(s_j + E_j - m'), with m' following
-// the largest s_j + E_j, beside the softmax's own exp2(s_j - m): fp16 weights lie in (2^-24, 2^15], and what falls below is less than 2^-31 of the largest term.  Queries are
-// held in fp16 relative to a power of two per row.  Roundings: weights to fp16 (2^-11), queries' and keys' elements below 2^-14 of their row's largest.
-// Bound: the instructions that unpack, not HBM (17/32 byte per element) and not the products (two of 8 cycles per 256 elements and scheduler): a stage of 32 keys
-// costs a warp some 450, at d = 128 a quarter of them decoding, most of the rest the same for every d.  256 sequences of 10^4 rows: d = 128 50.7 us (3.4 TB/s of codes and
-// scales that are read; values are the keys), d = 256 139 us, d = 64 with values of their own 59 us.  A warp has a ring of stages in shared memory, filled by
-// asynchronous copies of whole groups; quarter rows loaded to registers by the lanes that unpack them cost more addresses: 56 us, and 195 us at d = 256.
+// bf16, which holds every 4-bit value exactly.  Those registers are the A operand of scores^T [16 keys x 8 rows] = K Q^T (the order of the columns is the lanes' own, the same
+// for keys and queries) and, transposed 8 x 8 by movmatrix, of O^T [d x 8 rows] += V^T P^T, so a row is read and unpacked once where values are the keys.
+// Roundings: scores and sums are fp32 sums of exact products; a weight goes in as two bf16 numbers, together within 2^-17 of it.  (fp16 operands relative to a row's largest scale, that scale in the
+// row's weight, need fewer instructions: 256 x 10^4 keys 87 us against 99 at d = 128, 140 against 177 at d = 256, 119 against 157 with values of their own; but fp16 then spans all columns
+// of a row and all rows of a sequence at once, and columns or rows 2^24 below the largest were lost.)
+// Bound: the instructions that unpack, not HBM (17/32 byte per element) and not the products.  256 sequences of 10^4 rows, one query row each: d = 32 64 us, d = 64 65 us, d = 128
+// 99 us, d = 256 177 us; values of their own d = 64 91 us, d = 128 157 us; one sequence of 200 rows 5.9 us.  A warp has a ring of stages in shared memory, filled by
+// asynchronous copies of whole groups.
 #include <cfloat>
 
 #include "aif_cache4_plan.cuh"
@@ -22,30 +21,17 @@ namespace {
 constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32;
 constexpr int kFewRows = 8;
 constexpr int kFewGroups = 16;    // groups of 16 rows of a unit
-constexpr float kWeightBias = 7.f;   // weights are 2^7 at the offset and may grow by 2^8
 
-__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
     uint32_t o;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(o) : "r"(x));
     return o;
 }
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b)
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi)
 {
     uint32_t o;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o) : "r"(a), "r"(b));
-    return o;
-}
-__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi)
-{
-    uint32_t o;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(hi), "f"(lo));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(hi), "f"(lo));
     return o;
 }
 
@@ -73,54 +59,43 @@ __device__ __forceinline__ void load_row(RowCodes<NB> &r, const uint8_t *codes, 
         }
     }
 }
-// Largest scale byte of the row.
+// The values of two quarter rows: words 4 i .. 4 i + 3 of a row's o are the pairs (0,4) (1,5) (2,6) (3,7) of code word i.  The lane's words t NB .. t NB + NB - 1 of the 4 NB of a row lie
+// in one block of four words, or (NB = 8) in two.  Large scales have a second factor (see UnpackScale): a branch of the whole warp.
 template <int NB>
-__device__ __forceinline__ uint32_t top_scale(const RowCodes<NB> &r)
+__device__ __forceinline__ void unpack_rows(const RowCodes<NB> *r, int t, uint32_t (*o)[4 * NB])
 {
-    auto of_word = [](uint32_t x) { return max(max(x & 255u, (x >> 8) & 255u), max((x >> 16) & 255u, x >> 24)); };
-    if constexpr (NB == 1) return r.sc[0];
-    if constexpr (NB == 2) return max(r.sc[0] & 255u, r.sc[0] >> 8);
-    if constexpr (NB == 4) return of_word(r.sc[0]);
-    if constexpr (NB == 8) return max(of_word(r.sc[0]), of_word(r.sc[1]));
-}
-// The same of the blocks that are numbers (separate values: a block of no numbers is one in its own columns only, so the row's weight stays finite).
-template <int NB>
-__device__ __forceinline__ uint32_t top_number(RowCodes<NB> r)
-{
+    constexpr int kScales = NB == 8 ? 2 : 1;
+    uint32_t byte[2][kScales];
+    bool two = false;
 #pragma unroll
-    for (int i = 0; i < (NB + 3) / 4; ++i)
+    for (int x = 0; x < 2; ++x) {
+        if constexpr (NB == 8) {
+            const uint32_t sc = (t & 2 ? r[x].sc[1] : r[x].sc[0]) >> (16 * (t & 1));
+            byte[x][0] = sc & 255u, byte[x][1] = (sc >> 8) & 255u;
+        } else {
+            byte[x][0] = (r[x].sc[0] >> (8 * (t * NB / 4))) & 255u;
+        }
 #pragma unroll
-        for (int b = 0; b < 32; b += 8)
-            if (((r.sc[i] >> b) & 255u) == kMxNan) r.sc[i] &= ~(255u << b);
-    return top_scale<NB>(r);
-}
-// fp16 pair of 2^(byte - top), 0 below 2^-24; NaN for a block that is none.
-__device__ __forceinline__ uint32_t relative_scale(uint32_t byte, uint32_t top)
-{
-    if (byte == kMxNan) return 0x7fff7fffu;
-    const float f = __uint_as_float((uint32_t)max((int)(127u + byte) - (int)top, 0) << 23);
-    return pack_f16x2(f, f);
-}
-// 2^(top - 127) (the smallest is subnormal), NaN for a row that is none.
-__device__ __forceinline__ float row_scale(uint32_t top) { return __uint_as_float(top == kMxNan ? 0x7fffffffu : max(top << 23, 1u << 22)); }
-// The quarter row's values over 2^(top - 127): words 4 i .. 4 i + 3 of o are the pairs of code word i.  The lane's words t NB .. t NB + NB - 1 of the 4 NB of a row lie in
-// one block of four words, or (NB = 8) in two.
-template <int NB>
-__device__ __forceinline__ void unpack_row(const RowCodes<NB> &r, uint32_t top, int t, uint32_t (&o)[4 * NB])
-{
-    uint32_t f[NB == 8 ? 2 : 1];
-    if constexpr (NB == 8) {
-        const uint32_t sc = (t & 2 ? r.sc[1] : r.sc[0]) >> (16 * (t & 1));
-        f[0] = relative_scale(sc & 255u, top), f[1] = relative_scale((sc >> 8) & 255u, top);
-    } else {
-        f[0] = relative_scale((r.sc[0] >> (8 * (t * NB / 4))) & 255u, top);
+        for (int i = 0; i < kScales; ++i) {
+            const UnpackScale s(byte[x][i]);
+            two |= s.two;
+#pragma unroll
+            for (int w = i * NB / kScales; w < (i + 1) * NB / kScales; ++w) {
+                const uint4 v = unpack8_first(r[x].w[w], s.first);
+                o[x][4 * w] = v.x, o[x][4 * w + 1] = v.y, o[x][4 * w + 2] = v.z, o[x][4 * w + 3] = v.w;
+            }
+        }
     }
+    if (__any_sync(0xffffffffu, two)) {
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-        uint32_t h[4];
-        mx_decode8_f16(r.w[i], h);
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[4 * i + k] = mul_f16x2(h[k], f[NB == 8 ? i / 4 : 0]);
+            for (int i = 0; i < kScales; ++i) {
+                const UnpackScale s(byte[x][i]);
+                const uint32_t factor = s.two ? s.second : 0x3f803f80u;
+#pragma unroll
+                for (int w = 4 * i * NB / kScales; w < 4 * (i + 1) * NB / kScales; ++w) o[x][w] = mul_bf16x2(o[x][w], factor);
+            }
     }
 }
 
@@ -167,16 +142,16 @@ __global__ void __launch_bounds__(kFewThreads, (FewCfg<NB, SHARED>::kBlocks)) k_
         const int sink_groups = e.sink_groups(), rest_group = (e.rest >> 4) - sink_groups;
         const int32_t *table = c.table + (size_t)max(e.seq, 0) * c.max_pages;
 
-        // Queries as B operand: lane (g, t) holds its quarter of the columns of row g.
-        uint32_t q[2 * KS], raw[2 * KS];
-        float q_scale = 0.f;   // of row g: scale x log2(e) x the power of two that its fp16 values are relative to
+        // Queries as B operand: lane (g, t) holds its quarter of the columns of row g, in the order of the unpacked codes.
+        uint32_t q[2 * KS];
         {
             const bool there = g < rows;
             const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(a.q) + row_at(a, e.row0, head, r0 + (there ? g : 0), a.q_stride, D) + t * (D / 4);
 #pragma unroll
             for (int i = 0; i < NB; ++i) {
                 const uint4 x = there ? __ldg(reinterpret_cast<const uint4 *>(src) + i) : make_uint4(0u, 0u, 0u, 0u);
-                raw[4 * i] = x.x, raw[4 * i + 1] = x.y, raw[4 * i + 2] = x.z, raw[4 * i + 3] = x.w;
+                q[4 * i] = __byte_perm(x.x, x.z, 0x5410), q[4 * i + 1] = __byte_perm(x.x, x.z, 0x7632);
+                q[4 * i + 2] = __byte_perm(x.y, x.w, 0x5410), q[4 * i + 3] = __byte_perm(x.y, x.w, 0x7632);
             }
         }
         // Stage n of this warp: groups first + n kStride and, if two, the one behind.  Where they lie and what of them is visible is worked out for 32 groups at a time, one to
@@ -238,25 +213,10 @@ __global__ void __launch_bounds__(kFewThreads, (FewCfg<NB, SHARED>::kBlocks)) k_
         };
 #pragma unroll 1
         for (int n = 0; n < F::kRing - 1; ++n) bring(n);
-        {
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < 2 * KS; ++i) top = max(top, max(raw[i] & 0x7fffu, (raw[i] >> 16) & 0x7fffu));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const uint32_t field = min(max(top >> 7, 1u), 253u);            // exponent field of the largest (253: its inverse is still a number)
-            const float inv = __uint_as_float((254u - field) << 23);
-            q_scale = a.scale_log2 * __uint_as_float(field << 23);
-#pragma unroll
-            for (int i = 0; i < 2 * KS; ++i) q[i] = pack_f16x2(__uint_as_float(raw[i] << 16) * inv, __uint_as_float(raw[i] & 0xffff0000u) * inv);
-        }
-        // scores come with the rows 2 t and 2 t + 1 to a lane
-        const float k2[2] = {__shfl_sync(0xffffffffu, q_scale, 8 * t), __shfl_sync(0xffffffffu, q_scale, 8 * t + 4)};
-
         float o[KS][4];
 #pragma unroll
         for (int s = 0; s < KS; ++s) o[s][0] = o[s][1] = o[s][2] = o[s][3] = 0.f;
-        float m[2] = {-FLT_MAX, -FLT_MAX}, mw[2] = {-FLT_MAX, -FLT_MAX}, l[2] = {0.f, 0.f};   // offsets of the weights' sum and of the values', per row
+        float m[2] = {-FLT_MAX, -FLT_MAX}, l[2] = {0.f, 0.f};   // of the rows 2 t and 2 t + 1, as the scores come to a lane
 
         int slot = 0;
         for (int n = 0; n < stages; ++n) {
@@ -266,19 +226,18 @@ __global__ void __launch_bounds__(kFewThreads, (FewCfg<NB, SHARED>::kBlocks)) k_
             __syncwarp();
             const unsigned char *stage = ring + slot * F::kStage + g * (D / 2), *stage_sc = ring + slot * F::kStage + F::kCodes + g * NB;
             slot = slot + 1 == F::kRing ? 0 : slot + 1;
-            uint32_t kf[G][2][4 * NB];                       // keys (then values) as fp16 pairs
-            RowCodes<NB> vc[SHARED ? 1 : G][2];
-            float scale[G][2], s[G][4], w[G][4], v_exp[G][2];
+            uint32_t kf[2 * G][4 * NB];                      // keys (then values) as bf16 pairs: rows g and g + 8 of each group
+            RowCodes<NB> kr[2 * G], vc[SHARED ? 1 : 2 * G];
+            float s[G][4];
             bool see[G][2];
 #pragma unroll
             for (int x = 0; x < G; ++x) {
                 const uint32_t sp = __shfl_sync(0xffffffffu, span_now, (n * G + x) & 31), lo = sp & 255u, hi = (sp >> 8) & 255u;
-                RowCodes<NB> kr[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    load_row<NB>(kr[h], stage + x * (F::kCodes + F::kScales) + 8 * h * (D / 2), stage_sc + x * (F::kCodes + F::kScales) + 8 * h * NB, t);
+                    load_row<NB>(kr[2 * x + h], stage + x * (F::kCodes + F::kScales) + 8 * h * (D / 2), stage_sc + x * (F::kCodes + F::kScales) + 8 * h * NB, t);
                     if constexpr (!SHARED)
-                        load_row<NB>(vc[x][h], stage + (G + x) * (F::kCodes + F::kScales) + 8 * h * (D / 2), stage_sc + (G + x) * (F::kCodes + F::kScales) + 8 * h * NB, t);
+                        load_row<NB>(vc[2 * x + h], stage + (G + x) * (F::kCodes + F::kScales) + 8 * h * (D / 2), stage_sc + (G + x) * (F::kCodes + F::kScales) + 8 * h * NB, t);
                     see[x][h] = g + 8 * h >= lo && g + 8 * h < hi;
                 }
                 if (sp != 16u << 8) {
@@ -288,83 +247,74 @@ __global__ void __launch_bounds__(kFewThreads, (FewCfg<NB, SHARED>::kBlocks)) k_
 #pragma unroll
                         for (int i = 0; i < (NB + 3) / 4; ++i) {
                             const uint32_t bad = NB == 1 ? 0xffu : NB == 2 ? 0xffffu : 0xffffffffu;
-                            kr[h].sc[i] = !see[x][h] ? 0u : sp >> 16 ? bad : kr[h].sc[i];
-                            if constexpr (!SHARED) vc[x][h].sc[i] = !see[x][h] ? 0u : vc[x][h].sc[i];
+                            kr[2 * x + h].sc[i] = !see[x][h] ? 0u : sp >> 16 ? bad : kr[2 * x + h].sc[i];
+                            if constexpr (!SHARED) vc[2 * x + h].sc[i] = !see[x][h] ? 0u : vc[2 * x + h].sc[i];
                         }
                 }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t top = top_scale<NB>(kr[h]);
-                    unpack_row<NB>(kr[h], top, t, kf[x][h]);
-                    scale[x][h] = row_scale(top);
-                    // the exponent of the values' scale
-                    uint32_t vtop = top;
-                    if constexpr (!SHARED) vtop = top_number<NB>(vc[x][h]);
-                    v_exp[x][h] = (float)(int)vtop;
-                }
             }
+#pragma unroll
+            for (int x = 0; x < G; ++x) unpack_rows<NB>(kr + 2 * x, t, kf + 2 * x);
             bool raise = false;
 #pragma unroll
             for (int x = 0; x < G; ++x) {
                 float s2[2][4] = {};   // two chains of products
 #pragma unroll
-                for (int i = 0; i < KS; ++i) mma_f16(s2[i & 1], kf[x][0][2 * i], kf[x][1][2 * i], kf[x][0][2 * i + 1], kf[x][1][2 * i + 1], q[2 * i], q[2 * i + 1]);
+                for (int i = 0; i < KS; ++i) mma_bf16(s2[i & 1], kf[2 * x][2 * i], kf[2 * x + 1][2 * i], kf[2 * x][2 * i + 1], kf[2 * x + 1][2 * i + 1], q[2 * i], q[2 * i + 1]);
                 // s[0], s[1]: key g, rows 2 t, 2 t + 1; s[2], s[3]: key g + 8
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    s[x][i] = see[x][i >> 1] ? (s2[0][i] + s2[1][i]) * (k2[i & 1] * scale[x][i >> 1]) : -INFINITY;
-                    w[x][i] = s[x][i] + v_exp[x][i >> 1];
-                    raise |= s[x][i] > m[i & 1] + 8.f || w[x][i] > mw[i & 1] + 8.f;
+                    s[x][i] = see[x][i >> 1] ? (s2[0][i] + s2[1][i]) * a.scale_log2 : -INFINITY;
+                    raise |= s[x][i] > m[i & 1] + 8.f;
                 }
             }
-            // the offsets follow the maxima only when those have grown by a factor of 2^8
+            // the offset follows the maximum only when that has grown by a factor of 2^8
             if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    float ms = -FLT_MAX, mv = -FLT_MAX;
+                    float ms = -FLT_MAX;
 #pragma unroll
-                    for (int x = 0; x < G; ++x) ms = fmaxf(ms, fmaxf(s[x][r], s[x][r + 2])), mv = fmaxf(mv, fmaxf(w[x][r], w[x][r + 2]));
+                    for (int x = 0; x < G; ++x) ms = fmaxf(ms, fmaxf(s[x][r], s[x][r + 2]));
 #pragma unroll
-                    for (int b = 4; b < 32; b <<= 1) ms = fmaxf(ms, __shfl_xor_sync(0xffffffffu, ms, b)), mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, b));
-                    ms = ms > m[r] + 8.f ? ms : m[r], mv = mv > mw[r] + 8.f ? mv : mw[r];
-                    const float f = fast_exp2(mw[r] - mv);
-                    l[r] *= fast_exp2(m[r] - ms);
-                    m[r] = ms, mw[r] = mv;
+                    for (int b = 4; b < 32; b <<= 1) ms = fmaxf(ms, __shfl_xor_sync(0xffffffffu, ms, b));
+                    ms = ms > m[r] + 8.f ? ms : m[r];
+                    const float f = fast_exp2(m[r] - ms);
+                    l[r] *= f, m[r] = ms;
 #pragma unroll
                     for (int i = 0; i < KS; ++i) o[i][r] *= f, o[i][r + 2] *= f;
                 }
             }
-            const float mb[2] = {kWeightBias - mw[0], kWeightBias - mw[1]};
 #pragma unroll
             for (int x = 0; x < G; ++x) {
+                uint32_t p[2][2];   // [upper, lower half of the weights][keys g, keys g + 8], as B operand
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    l[i & 1] += fast_exp2(s[x][i] - m[i & 1]);
-                    w[x][i] = fast_exp2(w[x][i] + mb[i & 1]);
+                for (int h = 0; h < 2; ++h) {
+                    const float w0 = fast_exp2(s[x][2 * h] - m[0]), w1 = fast_exp2(s[x][2 * h + 1] - m[1]);
+                    l[0] += w0, l[1] += w1;
+                    const uint32_t hi = pack_bf16x2(w0, w1);
+                    p[0][h] = transpose8(hi), p[1][h] = transpose8(pack_bf16x2(w0 - __uint_as_float(hi << 16), w1 - __uint_as_float(hi & 0xffff0000u)));
                 }
-                const uint32_t p0 = transpose8(pack_f16x2(w[x][0], w[x][1])), p1 = transpose8(pack_f16x2(w[x][2], w[x][3]));
-                if constexpr (!SHARED) {
+                if constexpr (!SHARED) unpack_rows<NB>(vc + 2 * x, t, kf + 2 * x);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) unpack_row<NB>(vc[x][h], top_number<NB>(vc[x][h]), t, kf[x][h]);
+                for (int i = 0; i < KS; ++i) {
+                    const uint32_t v0 = transpose8(kf[2 * x][2 * i]), v1 = transpose8(kf[2 * x][2 * i + 1]), v2 = transpose8(kf[2 * x + 1][2 * i]), v3 = transpose8(kf[2 * x + 1][2 * i + 1]);
+                    mma_bf16(o[i], v0, v1, v2, v3, p[0][0], p[0][1]);
+                    mma_bf16(o[i], v0, v1, v2, v3, p[1][0], p[1][1]);
                 }
-#pragma unroll
-                for (int i = 0; i < KS; ++i)
-                    mma_f16(o[i], transpose8(kf[x][0][2 * i]), transpose8(kf[x][0][2 * i + 1]), transpose8(kf[x][1][2 * i]), transpose8(kf[x][1][2 * i + 1]), p0, p1);
             }
         }
         cp_async_wait_all();
-        // O^T: o[i][0], [1]: rows 2 t, 2 t + 1 of the column that lane quarter g / 2 has as element g % 2 of its pair 2 i; o[i][2], [3]: of its pair 2 i + 1
+        // O^T: o[i][0], [1]: rows 2 t, 2 t + 1 of the column that lane quarter g / 2 has as element g % 2 of its pair 2 i (columns c and c + 4 of a code word's eight);
+        // o[i][2], [3]: of its pair 2 i + 1
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             float lt = l[r];
 #pragma unroll
             for (int b = 4; b < 32; b <<= 1) lt += __shfl_xor_sync(0xffffffffu, lt, b);
             float *to = smem + (warp * kFewRows + 2 * t + r) * (D + 2);
-            const float f = fast_exp2(mw[r] - kWeightBias - 127.f - m[r]);   // sums relative to the offset of the weights' sum
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
-                const int col = (g >> 1) * (D / 4) + (g & 1) + 4 * i;
-                to[col] = o[i][r] * f, to[col + 2] = o[i][r + 2] * f;
+                const int col = (g >> 1) * (D / 4) + (i >> 1) * 8 + (i & 1) * 2 + (g & 1) * 4;
+                to[col] = o[i][r], to[col + 1] = o[i][r + 2];
             }
             if (g == 0) to[D] = m[r], to[D + 1] = lt;
         }

@@ -222,14 +222,20 @@ struct UnpackScale {
         first = f | (f << 16), second = s | (s << 16);
     }
 };
-__device__ __forceinline__ uint4 unpack8(uint32_t w, const UnpackScale &s)
+// (times the first factor alone)
+__device__ __forceinline__ uint4 unpack8_first(uint32_t w, uint32_t first)
 {
     uint4 o;
     o.x = ((w << 12) & 0x80008000u) | ((w << 6) & 0x01c001c0u);
     o.y = ((w << 8) & 0x80008000u) | ((w << 2) & 0x01c001c0u);
     o.z = ((w << 4) & 0x80008000u) | ((w >> 2) & 0x01c001c0u);
     o.w = (w & 0x80008000u) | ((w >> 6) & 0x01c001c0u);
-    o.x = mul_bf16x2(o.x, s.first), o.y = mul_bf16x2(o.y, s.first), o.z = mul_bf16x2(o.z, s.first), o.w = mul_bf16x2(o.w, s.first);
+    o.x = mul_bf16x2(o.x, first), o.y = mul_bf16x2(o.y, first), o.z = mul_bf16x2(o.z, first), o.w = mul_bf16x2(o.w, first);
+    return o;
+}
+__device__ __forceinline__ uint4 unpack8(uint32_t w, const UnpackScale &s)
+{
+    uint4 o = unpack8_first(w, s.first);
     if (s.two) o.x = mul_bf16x2(o.x, s.second), o.y = mul_bf16x2(o.y, s.second), o.z = mul_bf16x2(o.z, s.second), o.w = mul_bf16x2(o.w, s.second);
     return o;
 }

@@ -41,11 +41,13 @@ KERNELS = [(torch.float32, 128, 1), (torch.float32, 64, 5), (torch.bfloat16, 32,
            (torch.bfloat16, 160, 7), (torch.bfloat16, 64, 100), (torch.bfloat16, 128, 300), (torch.bfloat16, 256, 60)]
 
 
-def hold(q, k, v, out, columns=slice(None)):
-    """out [rows, 1, d] of a call with scale 1 / sqrt(d) over all of k, v [keys, d] (float64) against the reference, in these columns."""
+def hold(q, k, v, out, columns=slice(None), scale=None):
+    """out [rows, 1, d] of a call over all of k, v [keys, d] (float64) against the reference, in these columns: scores are sums of d fp32 products, whatever the elements' magnitudes."""
     d = k.shape[1]
+    scale = scale or 1 / math.sqrt(d)
     for r in range(0, q.shape[0], max(1, q.shape[0] // 5)):
-        ref, spread, mass, reach = R.attention(q[r].double(), k, v, 1 / math.sqrt(d))
+        ref, spread, mass, _ = R.attention(q[r].double(), k, v, scale)
+        reach = float((q[r].double().abs() @ k.abs().T).max() * scale)
         bound = R.attention_bound(q.dtype, ref, spread, mass, reach, d)
         err = (out[r].double() - ref).abs()
         assert (err <= bound)[:, columns].all(), (r, (err / bound)[:, columns].max().item())
@@ -67,3 +69,51 @@ def test_a_block_of_values_that_is_no_number_spoils_its_columns_alone(dtype, d, 
     assert torch.equal(torch.isnan(out), spoilt.expand_as(out)) and c.poll_status() == 0
     kq, vq = R.quantise(k)[0][:, 0], torch.nan_to_num(R.quantise(v)[0][:, 0])
     hold(q, kq, vq, out, ~spoilt)
+
+
+@pytest.mark.parametrize("dtype, d, rows", [x for x in KERNELS if x[1] > 32])
+@pytest.mark.parametrize("shared", [True, False])
+@pytest.mark.parametrize("power", [-24, -30, -60])
+def test_columns_far_smaller_than_the_others(dtype, d, rows, shared, power):
+    """A block of 32 columns of every row 2^power of the rest: those columns of the output are as exact as the others."""
+    n = 150
+    g = torch.Generator(device="cuda").manual_seed(d)
+    x = [torch.randn(n, 1, d, generator=g, device="cuda") * 0.3 for _ in range(1 if shared else 2)]
+    x[-1][:, :, d - 32:] *= 2.0 ** power
+    c = B.Cache4(d=d, n_pages=12, page_rows=16, n_seqs=1, max_pages=12, shared=shared)
+    c.append(ids(0), offsets([n]), *x)
+    q = (torch.randn(rows, 1, d, generator=g, device="cuda") * 4).to(dtype)
+    out = c.attention(q, torch.empty_like(q), offsets=offsets([rows]))
+    k, v = [R.quantise(y)[0][:, 0] for y in (x[0], x[-1])]
+    hold(q, k, v, out)
+
+
+@pytest.mark.parametrize("dtype, d, rows", [x for x in KERNELS if x[1] > 32])
+@pytest.mark.parametrize("power", [20, 26, 34, 60])
+def test_one_row_with_a_block_far_larger_than_the_rest(dtype, d, rows, power):
+    """Values of their own: a row of ordinary weight has one block 2^power times everything else.  The other columns do not feel it."""
+    n = 150
+    g = torch.Generator(device="cuda").manual_seed(d + power)
+    k, v = [torch.randn(n, 1, d, generator=g, device="cuda") * 0.3 for _ in range(2)]
+    v[77, :, :32] *= 2.0 ** power
+    c = B.Cache4(d=d, n_pages=12, page_rows=16, n_seqs=1, max_pages=12, shared=False)
+    c.append(ids(0), offsets([n]), k, v)
+    q = (torch.randn(rows, 1, d, generator=g, device="cuda") * 4).to(dtype)
+    out = c.attention(q, torch.empty_like(q), offsets=offsets([rows]))
+    hold(q, R.quantise(k)[0][:, 0], R.quantise(v)[0][:, 0], out)
+
+
+@pytest.mark.parametrize("dtype, d, rows", [x for x in KERNELS if x[1] > 32])
+def test_queries_far_smaller_where_keys_are_larger(dtype, d, rows):
+    """Elements of a query 2^20 apart against keys 2^20 apart the other way round: both halves of a score count alike."""
+    n = 150
+    g = torch.Generator(device="cuda").manual_seed(d)
+    k, v = [torch.randn(n, 1, d, generator=g, device="cuda") * 0.3 for _ in range(2)]
+    q = torch.randn(rows, 1, d, generator=g, device="cuda") * 4
+    k[:, :, :32] *= 2.0 ** 20
+    q[:, :, :32] *= 2.0 ** -20
+    q = q.to(dtype)
+    c = B.Cache4(d=d, n_pages=12, page_rows=16, n_seqs=1, max_pages=12, shared=False)
+    c.append(ids(0), offsets([n]), k, v)
+    out = c.attention(q, torch.empty_like(q), offsets=offsets([rows]))
+    hold(q, R.quantise(k)[0][:, 0], R.quantise(v)[0][:, 0], out)
