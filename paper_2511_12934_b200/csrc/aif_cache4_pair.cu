@@ -12,7 +12,7 @@
 //   10-15     unpack keys and values, 32 rows of a block at a time in turn (two to a block): a thread takes a key row; the codes of its next one are
 //             in flight in registers meanwhile, and the page number of the one after that
 // The maximum costs the softmax a third of its time, so it is left out where it cannot matter: |q| (formed as the queries are brought) times a bound of |k| (from the
-// scales of a block's keys, as they are unpacked) bounds every score; up to 2^+-96 the exponentials need no offset, since neither fp32 sums nor bf16
+// scales of a block's keys, as they are unpacked) bounds every score; up to 2^+-82 the exponentials need no offset, since neither fp32 sums nor bf16
 // probabilities lose precision with magnitude.
 // Eight codes of a word come apart as the pairs (0,4) (1,5) (2,6) (3,7) with two shifts, two masks and a multiplication each; queries are put
 // into the same order as they are brought, and sums are taken out of it as they are stored.
@@ -47,9 +47,9 @@ struct PairCfg {
     static constexpr size_t kSmem = 1024 + kQBytes + kStages * kStageBytes + kOutBytes + 512 + 256 * 4 + kStages * 2 * 2 * 4;
 };
 
-// Scores up to 2^+-kFreeScore, offsets up to 2^+-kFreeOffset and values between 2^-24 and 2^8 (of the largest scale of a block) keep probabilities and sums
-// inside fp32's range whatever their number.
-constexpr float kFreeScore = 96.f, kFreeOffset = 4.f;
+// Where no maximum is taken, exponents of weights lie within +-kFreeScore, the offset within +-kFreeOffset, scales of values at or below 2^8: a weight is at most
+// 2^86, a value 6 x 2^8 < 2^10.6, a sequence 2^30 rows, so sums stay below 2^126.6, those of a tile's joined pieces among them.
+constexpr float kFreeScore = 82.f, kFreeOffset = 4.f;
 
 template <int D, bool SHARED>
 __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)

@@ -117,3 +117,15 @@ def test_queries_far_smaller_where_keys_are_larger(dtype, d, rows):
     c.append(ids(0), offsets([n]), k, v)
     out = c.attention(q, torch.empty_like(q), offsets=offsets([rows]))
     hold(q, R.quantise(k)[0][:, 0], R.quantise(v)[0][:, 0], out)
+
+
+def test_sums_of_millions_of_keys_stay_finite():
+    """2^23 keys of 1536, all with the same large score: the sums of weights without an offset may not leave fp32."""
+    n, d, rows = 1 << 23, 64, 40
+    c = B.Cache4(d=d, n_pages=8200, page_rows=1024, n_seqs=1, max_pages=8200)
+    x = torch.full((n, d), 1536.0, dtype=torch.bfloat16, device="cuda")
+    c.append(ids(0), offsets([n]), x)
+    for score in (95.0, 80.0, -95.0, 200.0):   # in powers of two
+        q = torch.full((rows, d), score / (1.4426950408889634 * 1536 * d) * math.sqrt(d), device="cuda").bfloat16()
+        out = c.attention(q, torch.empty_like(q), offsets=offsets([rows]))
+        assert (out == 1536).all(), score
