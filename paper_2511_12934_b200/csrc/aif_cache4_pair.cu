@@ -47,9 +47,11 @@ struct PairCfg {
     static constexpr size_t kSmem = 1024 + kQBytes + kStages * kStageBytes + kOutBytes + 512 + 256 * 4 + kStages * 2 * 2 * 4;
 };
 
-// Where no maximum is taken, exponents of weights lie within +-kFreeScore, the offset within +-kFreeOffset, scales of values at or below 2^8: a weight is at most
-// 2^86, a value 6 x 2^8 < 2^10.6, a sequence 2^30 rows, so sums stay below 2^126.6, those of a tile's joined pieces among them.
+// Where no maximum is taken, exponents of weights lie within +-kFreeScore, the offset within +-kFreeOffset, scales of values between 2^-36 and 2^8: a weight is at most
+// 2^86, a value 6 x 2^8 < 2^10.6, a sequence 2^30 rows, so sums stay below 2^126.6, those of a tile's joined pieces among them; and the product of a weight of
+// 2^-86 or more with a value of 2^-37 or more is no subnormal.  (Scales of 2^-127 do not count: their values are zero or within 2^-124 of it.)
 constexpr float kFreeScore = 82.f, kFreeOffset = 4.f;
+constexpr uint32_t kFreeLow = 127u - 36u, kFreeTop = 127u + 8u;   // scale bytes
 
 template <int D, bool SHARED>
 __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
@@ -65,7 +67,7 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(q_full + 2);
     volatile uint32_t *abort_flag = tmem_slot + 1;
     float *q_norm = reinterpret_cast<float *>(smOut + C::kOutBytes + 512);   // [256], squared
-    float2 *k_bound = reinterpret_cast<float2 *>(q_norm + 256);        // [stage][32 rows each]: largest sum of a row's squared scales, largest scale of the values
+    float2 *k_bound = reinterpret_cast<float2 *>(q_norm + 256);        // [stage][32 rows each]: largest sum of a row's squared scales; 0 where the values' scales allow weights of any size
     __shared__ PlanShared<C::kThreads> plan;
 
     const Cache4 &c = a.c;
@@ -233,9 +235,8 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
                     // the first half of the block's scores was asked for with the block before; the second comes while the first is at work
                     if (!(ok = bring_scores(gb))) break;
                     const float4 kb = *reinterpret_cast<const float4 *>(k_bound + (cb + (uint32_t)j) % kS * 2);
-                    const float vtop = fmaxf(kb.y, kb.w);
                     // a code is at most 6: |k|^2 <= 36 x 32 x the sum of its blocks' squared scales
-                    bool free = reach * 33.9411255f * sqrtf(fmaxf(kb.x, kb.z)) <= kFreeScore && fabsf(m_used) <= kFreeOffset && vtop >= 5.9604645e-8f && vtop <= 256.f;
+                    bool free = reach * 33.9411255f * sqrtf(fmaxf(kb.x, kb.z)) <= kFreeScore && fabsf(m_used) <= kFreeOffset && kb.y + kb.w == 0.f;
                     free = __all_sync(0xffffffffu, free);   // (NaN: not)
                     tmem_ld_wait();
                     tmem_ld32(ts + 32, *reinterpret_cast<uint32_t(*)[32]>(&sc[32]));
@@ -438,15 +439,18 @@ __global__ void __launch_bounds__(512, 1) k_att4_pair(const AttCall a)
                 if (begun) {
                     if (k == 0) {
                         // bounds of the rows
-                        float sum = 0.f, vtop = 0.f;
+                        float sum = 0.f;
+                        uint32_t top = 0u, low = ~0u;   // largest scale byte of the values, least that is not 0, less 1
 #pragma unroll
                         for (int b = 0; b < kBlk; ++b) {
                             const float f = mx_scale((next[0].sc >> (8 * b)) & 255u);
-                            sum = fmaf(f, f, sum), vtop = fmaxf(vtop, mx_scale((next[C::kKinds - 1].sc >> (8 * b)) & 255u));
+                            const uint32_t vb = (next[C::kKinds - 1].sc >> (8 * b)) & 255u;
+                            sum = fmaf(f, f, sum), top = max(top, vb), low = min(low, vb - 1u);
                         }
                         // (as integers: NaN stays the largest)
-                        const uint32_t st = __reduce_max_sync(0xffffffffu, __float_as_uint(sum)), vt = __reduce_max_sync(0xffffffffu, __float_as_uint(vtop));
-                        if (lane == 0) k_bound[s * 2 + (item & 1)] = make_float2(__uint_as_float(st), __uint_as_float(vt));
+                        const uint32_t st = __reduce_max_sync(0xffffffffu, __float_as_uint(sum));
+                        const bool fit = __all_sync(0xffffffffu, top <= kFreeTop && low >= kFreeLow - 1u);
+                        if (lane == 0) k_bound[s * 2 + (item & 1)] = make_float2(__uint_as_float(st), fit ? 0.f : 1.f);
                     }
                     // A block of 32 at a time, its codes moved to the front: a loop of a quarter of the instructions, since the warps of a multiprocessor's quarter run different
                     // code and wait for it (16 x 10^4 x 10^4, d = 128: 784 us against 916; with values of their own, 148 x 256 x 8192: 181 us against 213)

@@ -129,3 +129,19 @@ def test_sums_of_millions_of_keys_stay_finite():
         q = torch.full((rows, d), score / (1.4426950408889634 * 1536 * d) * math.sqrt(d), device="cuda").bfloat16()
         out = c.attention(q, torch.empty_like(q), offsets=offsets([rows]))
         assert (out == 1536).all(), score
+
+
+@pytest.mark.parametrize("dtype, d, rows", [x for x in KERNELS if x[1] > 32])
+@pytest.mark.parametrize("score, power", [(-90, -60), (-75, -45), (-60, -100), (40, 30), (75, 60)])
+def test_small_columns_where_all_scores_are_far_from_zero(dtype, d, rows, score, power):
+    """All scores near 2^score, a block of values 2^power of the rest: no product of weight and value may leave fp32."""
+    n = 100
+    g = torch.Generator(device="cuda").manual_seed(d)
+    k = torch.full((n, 1, d), 1.0, device="cuda")
+    v = torch.randn(n, 1, d, generator=g, device="cuda")
+    v[:, :, d - 32:] *= 2.0 ** power
+    c = B.Cache4(d=d, n_pages=12, page_rows=16, n_seqs=1, max_pages=12, shared=False)
+    c.append(ids(0), offsets([n]), k, v)
+    q = torch.full((rows, 1, d), score / 1.4426950408889634 / math.sqrt(d), device="cuda").to(dtype)
+    out = c.attention(q, torch.empty_like(q), offsets=offsets([rows]))
+    hold(q, R.quantise(k)[0][:, 0], R.quantise(v)[0][:, 0], out)
