@@ -388,11 +388,18 @@ typedef struct {
     int64_t out_stride;        /* elements, >= n */
     void *workspace;           /* with x: aif_mx4_workspace_bytes(m, k) bytes, 16-byte aligned, not shared with a call that may run at the same time */
     int64_t workspace_bytes;
-    uint32_t *status;          /* device status word (AIF_STATUS_TIMEOUT), or NULL */
+    uint32_t *status;          /* device status word (AIF_STATUS_TIMEOUT), or NULL: the device's own, see aif_mx4_poll */
     int32_t relu;              /* 1: act(y) = max(y, 0) */
     int32_t pad_;
 } aif_mx4_product;
 int aif_mx4_linear(const aif_mx4_product *p, aif_stream stream);
+
+/* Reads and clears the current device's status word for products without one of their own (synchronises `stream`; bits of calls on other streams are seen once those are
+ * through).  After AIF_STATUS_TIMEOUT the outputs of the products since the last call are not to be used.  bits: host. */
+int aif_mx4_poll(uint32_t *bits, aif_stream stream);
+
+/* Where that word lies, for programs that look at it from the device or copy it with their results. */
+int aif_mx4_status_word(uint32_t **word);
 
 /* ---- behaviour sequences in a cache of 4-bit pages ------------------------------------------------------------
  * The projected behaviour sequences of many users kept on the GPU between requests (Section 3.3's pre-cache), at 17/32 bytes per value: rows are quantised

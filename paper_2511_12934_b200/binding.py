@@ -113,7 +113,8 @@ EXPORTS = [
     "aif_user_precompute", "aif_user_release", "aif_user_request_key", "aif_user_state_export", "aif_user_state_export_bea", "aif_score",
     "aif_score_batch", "aif_score_host", "aif_score_batch_host", "aif_score_noalloc", "aif_gather_rows", "aif_gather_sidecars", "aif_poll_status", "aif_get_stats",
     "aif_set_kernel_timing", "aif_get_kernel_timing", "aif_kernel_launches", "aif_selftest_bounded_wait", "aif_strerror", "aif_last_error",
-    "aif_mx4_scale_bytes", "aif_mx4_quantize", "aif_mx4_dequantize", "aif_mx4_workspace_bytes", "aif_mx4_linear",
+    "aif_mx4_scale_bytes", "aif_mx4_quantize", "aif_mx4_dequantize", "aif_mx4_workspace_bytes", "aif_mx4_linear", "aif_mx4_poll",
+    "aif_mx4_status_word",
     "aif_cache4_scratch_ints", "aif_cache4_reset", "aif_cache4_append", "aif_cache4_fork", "aif_cache4_copy", "aif_cache4_free", "aif_cache4_compact",
     "aif_cache4_read", "aif_cache4_attention_workspace", "aif_cache4_attention", "aif_cache4_poll",
 ]
@@ -166,6 +167,8 @@ def load_library(path: Optional[str] = None):
     lib.aif_mx4_quantize.argtypes = [vp, i32, i64, i32, i64, vp, vp, vp]
     lib.aif_mx4_dequantize.argtypes = [vp, vp, i64, i32, vp, i32, i64, vp]
     lib.aif_mx4_linear.argtypes = [C.POINTER(aif_mx4_product), vp]
+    lib.aif_mx4_poll.argtypes = [C.POINTER(C.c_uint32), vp]
+    lib.aif_mx4_status_word.argtypes = [C.POINTER(vp)]
     lib.aif_cache4_scratch_ints.argtypes, lib.aif_cache4_scratch_ints.restype = [c4], i64
     lib.aif_cache4_reset.argtypes = [c4, vp]
     lib.aif_cache4_append.argtypes = [c4, i32, vp, vp, vp, vp, i32, i64, i64, vp]
@@ -572,7 +575,7 @@ def mx4_dequantize(m: Mx4, out: torch.Tensor, stream=None) -> torch.Tensor:
 def mx4_linear(x, w: Mx4, out: torch.Tensor, bias: Optional[torch.Tensor] = None, relu: bool = False, status: Optional[torch.Tensor] = None,
                stream=None) -> torch.Tensor:
     """out [m, n] = act(x w^T + bias): x [m, k] as a tensor of out's type (quantised on the way) or as an Mx4, w [n, k] an Mx4, bias float32 [n];
-    status: a uint32-sized int32 tensor that takes AIF_STATUS_TIMEOUT."""
+    status: a uint32-sized int32 tensor that takes AIF_STATUS_TIMEOUT (without one: see mx4_poll_status)."""
     device = _cuda_device(out, "out")
     _mx4_check(w, "w", device)
     (n, k), m = w.codes.shape, out.shape[0]
@@ -602,6 +605,16 @@ def mx4_linear(x, w: Mx4, out: torch.Tensor, bias: Optional[torch.Tensor] = None
             p.workspace, p.workspace_bytes = keep.data_ptr(), keep.numel()
         _check(lib.aif_mx4_linear(C.byref(p), at.raw), "aif_mx4_linear")
     return out
+
+
+def mx4_poll_status(device="cuda", stream=None) -> int:
+    """Status bits (STATUS_TIMEOUT) of the device's products without a status tensor since the last call; waits for the stream."""
+    device = torch.device(device)
+    device = torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+    bits = C.c_uint32()
+    with _Launch(device, stream) as at:
+        _check(load_library().aif_mx4_poll(C.byref(bits), at.raw), "aif_mx4_poll")
+    return int(bits.value)
 
 
 class Cache4:

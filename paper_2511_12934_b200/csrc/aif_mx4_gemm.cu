@@ -68,6 +68,10 @@ struct GemmCfg {
     static constexpr size_t kSmem = 1024 + kStages * kStageBytes + kOutBytes + 256 + 8 * 64 * 4;
 };
 
+// Status bits of the products that were given no word of their own.
+__device__ uint32_t g_product_status;
+__global__ void k_clear_status(uint32_t bits) { atomicAnd(&g_product_status, ~bits); }
+
 struct GemmParams {
     int64_t m;
     int32_t n, k;
@@ -79,7 +83,7 @@ struct GemmParams {
     int32_t wide;        // rows of `out` begin and end on 16-byte boundaries: tile stores
     int32_t n_tiles;     // column tiles
     int64_t tiles;       // all (of the kernel that quantises too: bands of rows)
-    uint32_t *status;
+    uint32_t *status;    // or nullptr: g_product_status
 };
 
 __device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b)
@@ -282,7 +286,7 @@ __global__ void __launch_bounds__(GemmCfg::kThreads, 1) k_mx4_gemm(const __grid_
     }
 
     if (*abort_flag) {
-        if (tid == 0 && p.status) atomicOr(p.status, AIF_STATUS_TIMEOUT);
+        if (tid == 0) atomicOr(p.status ? p.status : &g_product_status, AIF_STATUS_TIMEOUT);
         const long long t0 = clock64();
         while (clock64() - t0 < 2000000ll) __nanosleep(1000);   // copies in flight land before the memory is given up
     }
@@ -485,7 +489,7 @@ __global__ void __launch_bounds__(NarrowCfg::kThreads, 1) k_mx4_narrow(const __g
     }
 
     if (*abort_flag) {
-        if (tid == 0 && p.status) atomicOr(p.status, AIF_STATUS_TIMEOUT);
+        if (tid == 0) atomicOr(p.status ? p.status : &g_product_status, AIF_STATUS_TIMEOUT);
         const long long t0 = clock64();
         while (clock64() - t0 < 2000000ll) __nanosleep(1000);   // copies in flight land before the memory is given up
     }
@@ -566,6 +570,16 @@ bool use_narrow(const aif_mx4_product &q, int el)
     return can && (el == 2 || w <= 76 * 1024) && (q.k * el <= 512 || q.m > 2 * 147 * kBM);
 }
 
+int product_result(cudaError_t e, const char *what)
+{
+    if (e == cudaSuccess) return AIF_OK;
+    char text[256];
+    snprintf(text, sizeof(text), "%s: %s", what, cudaGetErrorString(e));
+    cudaGetLastError();
+    set_last_error(text);
+    return AIF_ERR_CUDA;
+}
+
 }  // namespace
 }  // namespace aif
 
@@ -616,12 +630,33 @@ int aif_mx4_linear(const aif_mx4_product *q, aif_stream stream)
         e = q->dtype == AIF_BF16 ? run_narrow<__nv_bfloat16>(p, q->x, q->x_stride, q->w_codes, st) : run_narrow<float>(p, q->x, q->x_stride, q->w_codes, st);
     else if (e == cudaSuccess)
         e = q->dtype == AIF_BF16 ? run_gemm<__nv_bfloat16>(p, codes, q->w_codes, st) : run_gemm<float>(p, codes, q->w_codes, st);
-    if (e == cudaSuccess) return AIF_OK;
-    char text[256];
-    snprintf(text, sizeof(text), "aif_mx4_linear: %s", cudaGetErrorString(e));
-    cudaGetLastError();
-    set_last_error(text);
-    return AIF_ERR_CUDA;
+    return product_result(e, "aif_mx4_linear");
+}
+
+int aif_mx4_poll(uint32_t *bits, aif_stream stream)
+{
+    if (!bits) return AIF_ERR_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    uint32_t got = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&got, g_product_status, 4, 0, cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e == cudaSuccess && got != 0) {   // those bits alone: calls on other streams may set some meanwhile
+        k_clear_status<<<1, 1, 0, st>>>(got);
+        count_launch();
+        e = cudaGetLastError();
+        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    }
+    if (e == cudaSuccess) *bits = got;
+    return product_result(e, "aif_mx4_poll");
+}
+
+int aif_mx4_status_word(uint32_t **word)
+{
+    if (!word) return AIF_ERR_ARG;
+    void *at = nullptr;
+    const cudaError_t e = cudaGetSymbolAddress(&at, g_product_status);
+    if (e == cudaSuccess) *word = static_cast<uint32_t *>(at);
+    return product_result(e, "aif_mx4_status_word");
 }
 
 }  // extern "C"
