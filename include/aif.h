@@ -411,8 +411,8 @@ int aif_mx4_status_word(uint32_t **word);
  * sequences (aif_cache4_fork): refs counts the table entries that name it.  Pages without any stand in free_pages[0 .. n_free), are
  * handed out from its end, and return to it in the opposite order, so that the same calls on the same cache give the same pages.
  * What only the GPU can see sets a bit in *status.  It leaves the entry of the call undone: AIF_STATUS_BAD_ID for a sequence outside the cache or one
- * listed twice (the first stands), AIF_STATUS_FULL where pages or a sequence's table have no room.  It leaves the whole call undone: AIF_STATUS_BAD_ID
- * for offsets that descend or leave the rows given. */
+ * listed twice (the first stands), AIF_STATUS_FULL where pages or a sequence's table have no room (but see aif_cache4_copy: the destination is empty then).  It leaves the whole
+ * call undone: AIF_STATUS_BAD_ID for offsets that descend or leave the rows given. */
 typedef struct {
     uint32_t struct_size;
     int32_t d;                 /* width of a head: a multiple of 32, <= 256 */
@@ -447,7 +447,9 @@ int aif_cache4_append(const aif_cache4 *c, int32_t n, const int32_t *seq_ids, co
 
 /* Sequence dst[i] becomes sequence src[i], on the same pages (fork) or on pages of its own with the same contents (copy); what
  * it was before is freed first.  A snapshot for the requests in flight while rows are appended to src (the consistency that Section 3.4 asks
- * for).  src, dst: device int32 [n]; dst distinct, and no src among them (AIF_STATUS_BAD_ID, the entry is left undone). */
+ * for).  src, dst: device int32 [n]; dst distinct, and no src among them (AIF_STATUS_BAD_ID, the entry is left undone).  Copies take the free pages and those that the call's
+ * destinations give back, in the order of the entries; from the first one on that finds too few, copies that need any set AIF_STATUS_FULL, and their destinations are left EMPTY:
+ * what those were has been freed by then. */
 int aif_cache4_fork(const aif_cache4 *c, int32_t n, const int32_t *src, const int32_t *dst, aif_stream stream);
 int aif_cache4_copy(const aif_cache4 *c, int32_t n, const int32_t *src, const int32_t *dst, aif_stream stream);
 

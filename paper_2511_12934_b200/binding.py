@@ -699,7 +699,7 @@ class Cache4:
         self._share(self.lib.aif_cache4_fork, src, dst, stream)
 
     def copy(self, src: torch.Tensor, dst: torch.Tensor, stream=None):
-        """Sequence dst[i] becomes a copy of src[i] on pages of its own."""
+        """Sequence dst[i] becomes a copy of src[i] on pages of its own.  Without room for it dst[i] is left empty (STATUS_FULL)."""
         self._share(self.lib.aif_cache4_copy, src, dst, stream)
 
     def free(self, seq_ids: torch.Tensor, stream=None):

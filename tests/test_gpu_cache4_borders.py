@@ -145,3 +145,16 @@ def test_small_columns_where_all_scores_are_far_from_zero(dtype, d, rows, score,
     q = torch.full((rows, 1, d), score / 1.4426950408889634 / math.sqrt(d), device="cuda").to(dtype)
     out = c.attention(q, torch.empty_like(q), offsets=offsets([rows]))
     hold(q, R.quantise(k)[0][:, 0], R.quantise(v)[0][:, 0], out)
+
+
+@pytest.mark.parametrize("max_pages", [4, 20000])   # one CTA, one cluster
+def test_a_copy_without_room_leaves_its_destination_empty(max_pages):
+    """Two copies of three pages each where five are to be had: the first is served, the destination of the second has lost its page and has no row; a copy of nothing is served all the same."""
+    c = B.Cache4(d=32, n_pages=8, page_rows=16, n_seqs=6, max_pages=max_pages)
+    c.append(ids(0, 3), offsets([40, 16]), torch.randn(56, 32, device="cuda"))   # pages 0 .. 2 and 3; 4 .. 7 are free
+    c.copy(ids(0, 0, 5), ids(2, 3, 4))
+    assert c.poll_status() == B.STATUS_FULL
+    assert c.lengths.tolist() == [40, 0, 40, 0, 0, 0] and c.table[3].tolist() == [-1] * c.max_pages
+    assert c.n_free.item() == 2 and c.refs.sum().item() == 6
+    c.append(ids(3), offsets([32]), torch.randn(32, 32, device="cuda"))   # it can be used again
+    assert c.poll_status() == 0 and c.lengths[3].item() == 32 and c.n_free.item() == 0
