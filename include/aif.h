@@ -457,8 +457,8 @@ int aif_cache4_copy(const aif_cache4 *c, int32_t n, const int32_t *src, const in
 int aif_cache4_free(const aif_cache4 *c, int32_t n, const int32_t *seq_ids, aif_stream stream);
 
 /* All sequences of c into the cache `into` (of the same d, heads, shared, page_rows, n_seqs and max_pages, any n_pages; no buffer in common), whose former contents
- * are dropped: the pages in use take the pages 0, 1, ... in their order, shared ones stay shared.  c is left as it is.  With too
- * few pages `into` is left empty, with AIF_STATUS_FULL in its status. */
+ * are dropped: the pages in use take the pages 0, 1, ... in their order, shared ones stay shared.  c is left as it is but for its scratch, so two compactions of one cache do not
+ * run at the same time.  With too few pages `into` is left empty, with AIF_STATUS_FULL in its status. */
 int aif_cache4_compact(const aif_cache4 *c, const aif_cache4 *into, aif_stream stream);
 
 /* The first offsets[i + 1] - offsets[i] rows of sequence seq_ids[i], as values, to rows offsets[i] .. of k_out (and v_out): e.g. the projected
@@ -470,7 +470,12 @@ int aif_cache4_read(const aif_cache4 *c, int32_t n, const int32_t *seq_ids, cons
 /* Attention of query rows over the sequences of a cache (Section 4.2's target attention, eq. 3's profile attention):
  *   out = sum_j p_j v_j,   p = softmax_j(scale q k_j)   over the rows j of the sequence that are visible:
  * all of them, or with window > 0 the last `window` rows and the first `sinks` ones.  Query head h attends to head h / (n_heads / heads) of the cache. A
- * sequence without rows gives zero rows; one with a bad id, length or page gives NaN and AIF_STATUS_BAD_ID. */
+ * sequence without rows gives zero rows; one with a bad id, length or page gives NaN and AIF_STATUS_BAD_ID.
+ *
+ * Keys and values count exactly, whatever their magnitudes; scores and sums are fp32, and the output is rounded once.  Weights are fp32 in fp32 calls.  In bf16 calls they
+ * depend on the rows (queries x heads of a group) that a sequence of the call has on average: up to 32 within 2^-16 of themselves (fp32 where d is not 32, 64, 128 or 256), above
+ * that rounded to bf16 for d = 64, 128 and 256 (half a step: 2^-8 of each; their sum is of the rounded ones).  The same row and sequence can so give other last bits in another call; the same
+ * call gives the same bits.  Sums are of weights that are not divided yet, up to 2^8 each: values beyond 2^89 may overflow in them. */
 typedef struct {
     uint32_t struct_size;
     int32_t dtype;             /* of q and out */

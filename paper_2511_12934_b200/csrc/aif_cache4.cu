@@ -4,8 +4,9 @@
 // moves them, bound by HBM.  The books are kept by one CTA, or for many pages one cluster of CTAs: its phases hand over through
 // barriers, a matter of a microsecond, where separate launches would cost two or three each.  Nothing depends on the order of atomics: pages are
 // handed out and taken back by position in the call (prefix sums), so the same calls leave the same books.
-// Fork of 48 sequences 10.6 us (phases of one CTA, each some loads that need one another), freeing 3135 pages 21 us (30 thousand scattered accesses of one multiprocessor),
-// append of 200 thousand rows (d = 128, bf16) 23 us, 3 TB/s; moving the pages of 100 sequences 23 us.
+// Fork of 48 sequences 9.3 us (phases of one CTA, each some loads that need one another), freeing 3135 pages 21 us (30 thousand scattered accesses of one multiprocessor),
+// append of 200 thousand rows (d = 128) with the books of append and free 39 us in bf16, 47 in fp32 (13 of them books of no rows); read of as many 18 and 32 us;
+// copy and free of 100 sequences of 2000 rows 29 us, fork and free 23; compaction of those 14.5.
 #include <algorithm>
 #include <cstdio>
 
@@ -811,7 +812,11 @@ template <int OP>
 cudaError_t run_books(const BooksParams &p, cudaStream_t st)
 {
     count_launch();
-    // A few sequences: one CTA, 10.6 us against 12.6 (48 sequences of 32 pages forked), until its 32 warps have some hundred pages each.
+    // A few sequences: one CTA, until its 32 warps have some hundred pages each.  us of one CTA and of the cluster, over sequences that share their pages (fork), and with pages taken and
+    // given back (append and free of rows, both calls):
+    //   sequences x pages  16 x 32     48 x 32     64 x 49     100 x 60    128 x 80    16 x 200    16 x 1000   4 x 4000
+    //   fork               5.7   9.9   9.3  11.0   14.1  13.5  21.6  13.4  27.8  15.4  15.5  23.0  49    74    149   234
+    //   append + free      13.1  20.6  17.5 21.2   22.6  24.9  32.2  25.7  39.1  28.7  22.1  34.4  56    89    157   254
     if (p.n <= kFewSeqs && (int64_t)p.n * p.c.max_pages <= 32768) {
         k_books_few<OP><<<1, kFewThreads, 0, st>>>(p);
         return cudaGetLastError();

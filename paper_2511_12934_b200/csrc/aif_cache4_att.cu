@@ -6,8 +6,10 @@
 // the one at work.  A key row is spread over P lanes (32 of its elements, one block, to a lane for one query row; 16 elements where R rows share the decoding), 32 / P
 // keys to a step, each key group of lanes with a running maximum, weight and sum of its own, so a step needs no exchange but the score's sum over P lanes.
 // Codes are decoded once for score and sum where values are the keys; sums are fp32 throughout (f32x2 fused multiply-adds on register pairs).
-// Bound: issue slots (about three instructions per element of one row) before HBM (17/32 byte per element).  256 sequences of 10^4 rows: fp32 d = 128 166 us, bf16
-// d = 96 117 us; 1000 rows of one sequence with 50 keys, fp32 d = 64: 10.7 us.
+// Bound: issue slots (about three instructions per element of one row; 55 % of them taken, HBM 19 %).  256 sequences of 10^4 rows: fp32 d = 128 161 us, bf16 d = 96 117 us.
+// Many rows are not what it is for: keys are decoded again for every four rows, a CTA's tiles follow one another with nothing in flight between them, and the four-row forms spill
+// (334 to 554 bytes of stores a thread at 168 registers; the one-row forms spill nothing).  fp32, d = 64, one sequence of 50 keys: 1000 rows 10.9 us, 10^4 44 us,
+// 10^5 386 us; bf16, d = 96, 16 x 1000 rows x 10^4 keys 5.0 ms.
 #include <algorithm>
 #include <cfloat>
 #include <cstdio>
@@ -367,6 +369,15 @@ struct AttForm {
 // The tensor-core kernels: pieces of a cut tile have eight blocks (of some 1.2 us) on average at least, since a piece costs its queries, its record and its part of the join: 16
 // sequences of 1000 rows with 1000 keys (d = 128) 35 us against 45 with pieces of four, 64 of 128 rows with 1000 keys (d = 256) 37 us against 60; one of 256 rows with 1000
 // keys 28 us against 25.
+// Few or many rows, at 32 (the lengths are on the device): where the border would be best depends on what the call fills.  us of the kernel of few rows and of the one of many, on one box:
+//   rows per sequence          16          32          64
+//   16 x 1000 keys, d = 128    12.4  20.2  14.3  20.2  19.9  21.0
+//   16 x 10^4, d = 128         26.7  32.4  36.4  32.9  58.6  34.5
+//   148 x 10^4, d = 128        112   149   209   149   405   148
+//   148 x 10^4, d = 64         72    121   134   121   259   121
+//   148 x 10^4, d = 256        195   207   384   208   759   210
+//   148 x 10^4, d = 128, own   180   171   340   171   664   172
+//   1 x 1000, d = 128          10.7  19.5  10.8  19.8  10.8  20.2
 AttForm kernel_of(const aif_cache4 *c, const aif_cache4_query *q)
 {
     const int64_t group = q->n_heads / c->heads, per_seq = (q->rows + q->n - 1) / q->n * group;   // query rows of a sequence and a head of the cache, on average

@@ -4,10 +4,10 @@
 // A warp takes 16 keys at a time, one group of 16 rows of a page.  Lane (g, t) = (lane / 4, lane % 4) reads a quarter of the rows g and g + 8 and unpacks it to
 // bf16, which holds every 4-bit value exactly.  Those registers are the A operand of scores^T [16 keys x 8 rows] = K Q^T (the order of the columns is the lanes' own, the same
 // for keys and queries) and, transposed 8 x 8 by movmatrix, of O^T [d x 8 rows] += V^T P^T, so a row is read and unpacked once where values are the keys.
-// Roundings: scores and sums are fp32 sums of exact products; a weight goes in as two bf16 numbers, together within 2^-17 of it.  (fp16 operands relative to a row's largest scale, that scale in the
+// Roundings: scores and sums are fp32 sums of exact products; a weight goes in as two bf16 numbers, together within 2^-16 of it.  (fp16 operands relative to a row's largest scale, that scale in the
 // row's weight, need fewer instructions: 256 x 10^4 keys 87 us against 99 at d = 128, 140 against 177 at d = 256, 119 against 157 with values of their own; but fp16 then spans all columns
 // of a row and all rows of a sequence at once, and columns or rows 2^24 below the largest were lost.)
-// Bound: the instructions that unpack, not HBM (17/32 byte per element) and not the products.  256 sequences of 10^4 rows, one query row each: d = 32 64 us, d = 64 65 us, d = 128
+// Bound: the instructions that unpack (at d = 128 issue slots 59 %, ALU 47 %), not HBM (22 %) and not the products (31 %).  256 sequences of 10^4 rows, one query row each: d = 32 64 us, d = 64 65 us, d = 128
 // 99 us, d = 256 177 us; values of their own d = 64 91 us, d = 128 157 us; one sequence of 200 rows 5.9 us.  A warp has a ring of stages in shared memory, filled by
 // asynchronous copies of whole groups.
 #include <cfloat>

@@ -16,11 +16,13 @@
 // probabilities lose precision with magnitude.
 // Eight codes of a word come apart as the pairs (0,4) (1,5) (2,6) (3,7) with two shifts, two masks and a multiplication each; queries are put
 // into the same order as they are brought, and sums are taken out of it as they are stored.
-// Bound: what the softmax warps issue and wait for (per 64 keys and half a tile 512 cycles of exponentials in a scheduler, some 1100 in all; a polynomial on other units in
-// place of a quarter or half of the exponentials gained nothing, half of the products left out 1 %), and instruction fetch: five kinds of code share a multiprocessor, so parts
-// stand once and cold ones aside.  16 x 10^4 rows x 10^4 keys, d = 128: 766 us, 1070 TFLOP/s; 148 x 256 x 8192: 151 us, d = 64 134 us, values of their own 181 us; one tile of two
-// blocks 17 us, of which 3 plan, 2.5 queries, 2.3 the output.
-// Rounding: probabilities are rounded to bf16 for the product (relative 2^-9 each), and their sum is of the rounded ones, everything else is fp32.
+// Bound: what the softmax warps issue and wait for, not one unit: issue slots 59 %, exponentials 51 %, products 50 % of the cycles, ALU 43 %; a scheduler's warps wait longest for
+// scores and probabilities on their way from and to tensor memory.  (A polynomial on other units in place of a quarter or half of the exponentials gained nothing, half of the products left out
+// 1 %.)  k_att_tc does the same sizes with bf16 keys in 672 us: it has no unpacking warps, and its Q K^T of block j + 2 does not wait for P V of block j, whose probabilities lie
+// in the columns of the scores here.  Instruction fetch: five kinds of code share a multiprocessor, so parts stand once and cold ones aside.
+// 16 x 10^4 rows x 10^4 keys, d = 128: 782 us, 1050 TFLOP/s; 148 x 256 x 8192: 161 us, d = 64 136 us, values of their own 180 us; one tile of two blocks 17 us, of which 3
+// plan, 2.5 queries, 2.3 the output.
+// Rounding: probabilities are rounded to bf16 for the product (relative 2^-8 each), and their sum is of the rounded ones, everything else is fp32.
 #include <cfloat>
 #include <type_traits>
 

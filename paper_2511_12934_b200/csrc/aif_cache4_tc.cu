@@ -12,9 +12,10 @@
 //          meanwhile, and the page numbers for the one after that
 // Eight codes of a word come apart as the pairs (0,4) (1,5) (2,6) (3,7) with two shifts, two masks and a multiplication each; queries are put
 // into the same order as they are brought, and sums are taken out of it as they are stored.
-// Bound: the unpacking warps and, with shared-memory operands of 64 keys x 256, the products: 148 tiles x 8192 keys 181 us (880 TFLOP/s; values of their own 326 us), 16 x 10^4 rows x
-// 10^4 keys 1.97 ms (832 TFLOP/s), one tile of two blocks 16 us.
-// Rounding: probabilities are rounded to bf16 for the product (relative 2^-9 each), and their sum is of the rounded ones, everything else is fp32.
+// Bound: no unit by itself (issue slots 55 %, ALU 43 %, products 41 % of the cycles, exponentials 21 %): one tile of 128 rows is at work, and its softmax, its products and the
+// unpacking of 64 keys x 256 wait for one another.  148 tiles x 8192 keys 180 us (880 TFLOP/s; values of their own 326 us), 16 x 10^4 rows x 10^4 keys 1.96 ms (832 TFLOP/s), one
+// tile of two blocks 16 us.
+// Rounding: probabilities are rounded to bf16 for the product (relative 2^-8 each), and their sum is of the rounded ones, everything else is fp32.
 #include <cfloat>
 
 #include "aif_cache4_plan.cuh"
